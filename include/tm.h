@@ -85,13 +85,15 @@ extern "C" {
 #define TM_ERR_WORKSPACE 8  /* workspace NULL, misaligned (256 bytes) or smaller than tm_workspace_bytes() */
 #define TM_ERR_TOO_LARGE 9  /* more matrices than the built-in scratch of tm_find_mask_batched_static() can serve */
 #define TM_ERR_CAPTURE 10   /* cuda_stream is being captured and the call would have to copy descriptor tables from host memory */
+#define TM_ERR_RANGE 11     /* a scalar out of range: list length, temperature, eps or scale */
 
 /* device status bits */
-#define TM_DEV_NONFINITE 1  /* an Inf or NaN was met in W (it is ordered by its bit pattern) */
+#define TM_DEV_NONFINITE 1  /* an Inf or NaN was met in W (it is ordered by its bit pattern); tm_top_logits: a NaN or +Inf */
 #define TM_DEV_INTERNAL 2   /* a bound inside a kernel was hit (not expected to happen).  An iteration cap of a per-block search leaves
                                that block with the mask reached so far; a bulk copy that did not land within its bounded wait makes
                                the warp stop, and the outputs of its remaining work items stay UNWRITTEN: treat the call as failed */
 #define TM_DEV_BADMASK 4    /* tm_compress_2_4: a group of four did not hold exactly two kept entries (zeros were emitted) */
+#define TM_DEV_BADID 8      /* tm_distill_*: an id beyond the vocabulary, or twice in one row (the entry was left out) */
 
 typedef struct tm_problem {
     const void* W;          /* device, dtype, rows x ld */
@@ -248,6 +250,69 @@ int tm_mask_violations(const void* W, int dtype, int64_t rows, int64_t cols, int
                        unsigned long long* violations_out, void* workspace_dev, size_t workspace_bytes, void* cuda_stream);
 int tm_compress_2_4(const void* W, int dtype, int64_t rows, int64_t cols, int64_t ld, const uint32_t* mask,
                     void* values, uint32_t* meta, void* values_t, uint32_t* meta_t, int* status_dev, void* cuda_stream);
+
+/*
+ * Operators of the training step around the masked layers: the normalisation between them, and the loss that ties a pruned
+ * network to the dense one it came from.  Matrices are row-major with a leading dimension in elements (any, rows need no
+ * alignment beyond that of an element: rows that start and end on 16-byte boundaries are the fast ones), fp32 or bf16; sums,
+ * statistics and exponentials are fp32 (losses are put together in fp64), and a result is rounded to bf16 once.  The calls run
+ * asynchronously on cuda_stream, never allocate, only launch kernels (they can be recorded by a stream capture) and give the
+ * same bits for the same input.  An output may lie exactly on an input of the same shape, type and leading dimension where that
+ * is said; any other overlap is not allowed.
+ *
+ * tm_layer_norm -- h = x + residual (residual NULL: h = x); over the columns of every row mu = mean(h),
+ * rstd = 1 / sqrt(mean((h - mu)^2) + eps), y = (h - mu) * rstd * weight + bias.  weight, bias: cols entries of weight_dtype, NULL
+ * for ones and zeros.  sum_out (may be NULL) receives h rounded to dtype, mean_out and rstd_out (rows floats each, may be NULL)
+ * the statistics; y comes from h before rounding.  y or sum_out may lie on x or residual.
+ *
+ * tm_layer_norm_backward -- with g = dy * weight and xh = (h - mean) * rstd:
+ *   dx = rstd * (g - mean_c(g) - xh * mean_c(g * xh)) + dsum,   dweight = sum_r(dy * xh),   dbias = sum_r(dy).
+ * h is the forward pass's x, or its sum_out; dx is the gradient of both its addends.  dsum (may be NULL) is a gradient that reaches
+ * h by another way (the residual stream of a pre-norm block).  dweight_out and dbias_out (cols entries of weight_dtype, either may be
+ * NULL) are written, not added to; they need a workspace of tm_layer_norm_workspace_bytes(rows, cols) bytes, 256-byte aligned.
+ * dx may lie on dy, h or dsum.
+ */
+int tm_layer_norm(const void* x, int64_t ld_x, const void* residual, int64_t ld_residual, int dtype, int64_t rows, int64_t cols,
+                  const void* weight, const void* bias, int weight_dtype, float eps, void* sum_out, int64_t ld_sum, void* y, int64_t ld_y,
+                  float* mean_out, float* rstd_out, void* cuda_stream);
+size_t tm_layer_norm_workspace_bytes(int64_t rows, int64_t cols);
+int tm_layer_norm_backward(const void* dy, int64_t ld_dy, const void* h, int64_t ld_h, int dtype, int64_t rows, int64_t cols,
+                           const void* weight, int weight_dtype, const float* mean, const float* rstd, const void* dsum, int64_t ld_dsum,
+                           void* dx, int64_t ld_dx, void* dweight_out, void* dbias_out, void* workspace_dev, size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * tm_top_logits -- the k largest logits of every row, largest first, equal ones by the lower id (1 <= k <= TM_TOP_MAX):
+ * values_out[rows][k] (fp32, not divided by the temperature), ids_out[rows][k]; where k > vocab the list ends in (-Inf, -1).
+ * -0 counts as 0, NaN is larger than everything.  lse_out (rows floats, may be NULL): log sum_j exp(logit_j / temperature) over the
+ * whole row.  -Inf (a masked logit) is an ordinary value; NaN and +Inf raise TM_DEV_NONFINITE in *status_dev (may be NULL).
+ *
+ * tm_distill_loss, tm_distill_grad, tm_distill_loss_grad -- Kullback-Leibler divergence of a student from such lists.  With
+ * q = softmax(logits / temperature) over a row and f = scale * row_weight[row] (NULL: 1):
+ *   teacher_lse NULL:  p = softmax(top_values / temperature) over the row's entries, p_rest = 0;
+ *   else:              p_k = exp(top_values_k / temperature - teacher_lse[row]) (the lse_out of tm_top_logits at the same temperature),
+ *                      p_rest = max(0, 1 - sum_k p_k), one class for all logits that are not listed, q_rest their sum;
+ *   loss = f * (sum_k p_k * (log p_k - log q_k) + p_rest * (log p_rest - log q_rest));
+ *   dlogits_j = f / temperature * (q_j - p_j) for a listed logit, f / temperature * (q_j - p_rest * q_j / q_rest) for another.
+ * Terms with p_k = 0 are left out, and so is that of p_rest where q_rest = 0.  An entry whose id is negative is padding (lists of different
+ * lengths); one whose id is not below vocab, or stood in the row before, is left out too and raises TM_DEV_BADID in *status_dev.
+ * A row of weight 0, or without entries, has loss 0 and gradient 0 whatever its logits hold.  0 <= k <= TM_TOP_MAX.
+ *   tm_distill_loss       loss_out[rows]; stats_out[rows][2] (may be NULL): log-sum-exp of logits / temperature, log q_rest (0 without teacher_lse)
+ *   tm_distill_grad       dlogits, from the stats of tm_distill_loss on the same arguments, times grad_loss[row] (NULL: 1)
+ *   tm_distill_loss_grad  both in one pass over the logits, for a step whose gradient of the loss is known (1 per row; a factor goes into scale)
+ * dlogits may lie on logits.
+ */
+#define TM_TOP_MAX 256
+int tm_top_logits(const void* logits, int dtype, int64_t rows, int64_t vocab, int64_t ld, int k, float temperature,
+                  float* values_out, int32_t* ids_out, float* lse_out, int* status_dev, void* cuda_stream);
+int tm_distill_loss(const void* logits, int dtype, int64_t rows, int64_t vocab, int64_t ld, const float* top_values, const int32_t* top_ids, int k,
+                    const float* teacher_lse, const float* row_weight, float temperature, float scale, float* loss_out, float* stats_out,
+                    int* status_dev, void* cuda_stream);
+int tm_distill_grad(const void* logits, int dtype, int64_t rows, int64_t vocab, int64_t ld, const float* top_values, const int32_t* top_ids, int k,
+                    const float* teacher_lse, const float* row_weight, float temperature, float scale, const float* stats, const float* grad_loss,
+                    void* dlogits, int64_t ld_d, int* status_dev, void* cuda_stream);
+int tm_distill_loss_grad(const void* logits, int dtype, int64_t rows, int64_t vocab, int64_t ld, const float* top_values, const int32_t* top_ids, int k,
+                         const float* teacher_lse, const float* row_weight, float temperature, float scale, float* loss_out, void* dlogits,
+                         int64_t ld_d, int* status_dev, void* cuda_stream);
 
 const char* tm_status_string(int code);
 int tm_version(void);

@@ -11,3 +11,7 @@ from .binding import (  # noqa: F401
     tm_version, tm_workspace_bytes, tm_aux_workspace_bytes, tm_nm_mask_1d, tm_mask_violations, tm_mask_hamming, tm_compress_2_4,
     TM_DEV_BADMASK, TM_NM1D_ABSORB_MEAN,
 )
+from .binding_train import (  # noqa: F401
+    TM_DEV_BADID, TM_ERR_RANGE, TM_TOP_MAX, tm_layer_norm, tm_layer_norm_backward, tm_layer_norm_workspace_bytes, tm_top_logits,
+    tm_distill_loss, tm_distill_grad, tm_distill_loss_grad,
+)

@@ -312,6 +312,13 @@ int static_scratch_address(void** out) {
 
 }  // namespace
 
+int tmask::device_sms(int* sms) {
+    DeviceState* d = nullptr;
+    const int rc = current_device(&d);
+    if (rc == TM_OK) *sms = d->sms;
+    return rc;
+}
+
 extern "C" {
 
 size_t tm_mask_words_per_row(int64_t cols) { return cols > 0 ? (size_t)((cols + 31) / 32) : 0; }
@@ -634,6 +641,7 @@ const char* tm_status_string(int code) {
     case TM_ERR_WORKSPACE: return "workspace missing, misaligned or too small";
     case TM_ERR_TOO_LARGE: return "too many matrices for the built-in scratch (TM_STATIC_MAX_MATRICES per call)";
     case TM_ERR_CAPTURE: return "the stream is being captured and the call would have to copy descriptor tables from host memory (use tm_plan_run)";
+    case TM_ERR_RANGE: return "a scalar is out of range (list length, temperature, eps or scale)";
     default: return "unknown status";
     }
 }

@@ -15,6 +15,7 @@ constexpr int kBF16 = 1;
 constexpr int kDevNonFinite = 1;
 constexpr int kDevInternal = 2;
 constexpr int kDevBadMask = 4;
+constexpr int kDevBadId = 8;
 
 // One matrix of a (possibly batched) call, as the kernels see it.
 struct DevProblem {

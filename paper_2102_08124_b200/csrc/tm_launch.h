@@ -90,4 +90,59 @@ cudaError_t launch_compress24_stream(const AuxProblem& P, void* values, uint32_t
 cudaError_t launch_compress24(const AuxProblem& P, void* values, uint32_t* meta, void* values_t, uint32_t* meta_t, int* status,
                               int sms, cudaStream_t stream);
 
+// Operators of the training step around the masked layers.  Row strides (ld_*) are in elements; pointers marked "or null" are optional.
+struct NormArgs {                               // tm_kernels_norm.cu
+    const void *x, *residual;                   // residual or null
+    long long rows, cols, ld_x, ld_residual, ld_sum, ld_y;
+    const void *weight, *bias;                  // or null
+    bool weight_f32, weight_vec, bias_vec;      // parameters are fp32 (else bf16); may be read 16 bytes at a time (set by the launch)
+    float eps;
+    void *sum, *y;                              // sum or null
+    float *mean, *rstd;                         // or null
+};
+struct NormBackArgs {
+    const void *dy, *h, *dsum;                  // dsum or null
+    long long rows, cols, ld_dy, ld_h, ld_dsum, ld_dx;
+    const void* weight;                         // or null
+    bool weight_f32, weight_vec;
+    const float *mean, *rstd;
+    void* dx;
+    float* partials;                            // norm_partial_rows() rows of 2 cols floats, or null
+};
+int norm_partial_rows(long long rows, long long cols);
+cudaError_t launch_norm_forward(NormArgs a, int dtype, int sms, cudaStream_t stream);
+cudaError_t launch_norm_backward(NormBackArgs a, int dtype, void* dweight, void* dbias, int sms, cudaStream_t stream);
+
+constexpr int kTopMax = 256;                    // longest list of largest logits
+struct TopArgs {                                // tm_kernels_top.cu
+    const void* logits;
+    long long rows, vocab, ld;
+    int k;
+    float temperature;
+    float* values;
+    int* ids;
+    float* lse;                                 // or null
+    int* status;                                // or null
+};
+cudaError_t launch_top(const TopArgs& a, int dtype, int sms, cudaStream_t stream);
+
+struct DistillArgs {                            // tm_kernels_distill.cu
+    const void* logits;
+    long long rows, vocab, ld, ld_d;
+    const float* values;
+    const int* ids;
+    int k;
+    const float *teacher_lse, *row_weight;      // or null
+    float temperature, scale;
+    float* loss;
+    float* stats;                               // written by the loss (or null there), read by the gradient alone
+    const float* grad_loss;                     // or null
+    void* dlogits;
+    int* status;                                // or null
+};
+cudaError_t launch_distill(const DistillArgs& a, int dtype, bool loss, bool grad, int sms, cudaStream_t stream);
+
+// The current device's number of multiprocessors (looked up once per device); a TM_* code.
+int device_sms(int* sms);
+
 }  // namespace tmask
