@@ -302,6 +302,7 @@ int tm_layer_norm_backward(const void* dy, int64_t ld_dy, const void* h, int64_t
  * dlogits may lie on logits.
  */
 #define TM_TOP_MAX 256
+#define TM_VOCAB_MAX (1 << 22)   /* columns of a logit matrix */
 int tm_top_logits(const void* logits, int dtype, int64_t rows, int64_t vocab, int64_t ld, int k, float temperature,
                   float* values_out, int32_t* ids_out, float* lse_out, int* status_dev, void* cuda_stream);
 int tm_distill_loss(const void* logits, int dtype, int64_t rows, int64_t vocab, int64_t ld, const float* top_values, const int32_t* top_ids, int k,

@@ -16,11 +16,14 @@ TM_ERR_RANGE = 11
 TM_TOP_MAX = 256
 
 _ready = None
+_torch = None              # torch, once a call needed it: importing this package alone does not import torch
+_raw_stream = None
 
 
 def _lib():
-    global _ready
+    global _ready, _torch, _raw_stream
     if _ready is None:
+        import torch
         lib = binding.load_library()
         vp, i32, i64, sz, f32 = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_size_t, ctypes.c_float
         lib.tm_layer_norm.argtypes = [vp, i64, vp, i64, i32, i64, i64, vp, vp, i32, f32, vp, i64, vp, i64, vp, vp, vp]
@@ -33,60 +36,73 @@ def _lib():
         lib.tm_distill_loss_grad.argtypes = lists + [vp, vp, i64, vp, vp]
         for f in (lib.tm_layer_norm, lib.tm_layer_norm_backward, lib.tm_top_logits, lib.tm_distill_loss, lib.tm_distill_grad, lib.tm_distill_loss_grad):
             f.restype = i32
+        _torch = torch
+        # the address of the current stream without a Stream object around it (2 us less a call), where this torch has it
+        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
         _ready = lib
     return _ready
 
 
 def _call(fn, device, stream, *args):
     """fn(*args, stream) with `device` current."""
-    import torch
-    s = (stream if stream is not None else torch.cuda.current_stream(device)).cuda_stream
-    if torch.cuda.current_device() == device.index:
+    index = device.index
+    s = stream.cuda_stream if stream is not None else _raw_stream(index)
+    if _torch.cuda.current_device() == index:
         rc = fn(*args, s)
     else:
-        with torch.cuda.device(device):
+        with _torch.cuda.device(device):
             rc = fn(*args, s)
     if rc != 0:
         raise TmError(rc, binding.tm_status_string(rc))
 
 
-def _matrix(t, what, like=None):
-    """Checks a 2-D matrix (of the shape, type and device of `like`); returns its leading dimension."""
-    if t.dim() != 2 or not t.is_cuda or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise TmError(2, "%s must be a 2-D CUDA tensor with unit column stride" % what)
-    if like is not None and (t.shape != like.shape or t.dtype != like.dtype or t.device != like.device):
+def _input(t, what):
+    """Checks the matrix of a call; returns its type's code, device, shape and leading dimension."""
+    code = 1 if t.dtype is _torch.bfloat16 else 0 if t.dtype is _torch.float32 else -1
+    if code < 0:
+        raise TmError(5, "%s must be float32 or bfloat16" % what)
+    if not t.is_cuda or t.dim() != 2:
+        raise TmError(2, "%s must be a 2-D CUDA tensor" % what)
+    rows, cols = t.shape
+    step = t.stride()
+    if cols > 1 and step[1] != 1:
+        raise TmError(2, "%s must have unit column stride" % what)
+    return code, t.device, rows, cols, step[0] if rows > 1 else cols
+
+
+def _other(t, what, like):
+    """Checks a matrix of the shape, type and device of `like`; returns its leading dimension."""
+    if t.shape != like.shape or t.dtype is not like.dtype or t.device != like.device:
         raise TmError(2, "%s must have the shape, dtype and device of the input matrix" % what)
     rows, cols = t.shape
-    return t.stride(0) if rows > 1 else cols
+    step = t.stride()
+    if cols > 1 and step[1] != 1:
+        raise TmError(2, "%s must have unit column stride" % what)
+    return step[0] if rows > 1 else cols
 
 
 def _array(t, shape, dtype, device, what):
     """Checks a small contiguous array; returns its address, or None for None."""
     if t is None:
         return None
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise TmError(5, "%s must be %s" % (what, dtype))
-    if tuple(t.shape) != shape or t.device != device or not t.is_contiguous():
+    if t.shape != shape or t.device != device or not t.is_contiguous():
         raise TmError(2, "%s must be a contiguous tensor of shape %s on the matrix's device" % (what, shape))
     return t.data_ptr()
 
 
 def _params(weight, bias, cols, device, default):
-    import torch
     kind = weight.dtype if weight is not None else bias.dtype if bias is not None else default
-    code = 0 if kind == torch.float32 else 1 if kind == torch.bfloat16 else None
-    if code is None:
+    code = 1 if kind is _torch.bfloat16 else 0 if kind is _torch.float32 else -1
+    if code < 0:
         raise TmError(5, "weight and bias must be float32 or bfloat16")
     return kind, code, _array(weight, (cols,), kind, device, "weight"), _array(bias, (cols,), kind, device, "bias")
 
 
-def _code(t, what):
-    import torch
-    if t.dtype == torch.bfloat16:
-        return 1
-    if t.dtype == torch.float32:
-        return 0
-    raise TmError(5, "%s must be float32 or bfloat16" % what)
+def _like(t):
+    """An output matrix: the shape of `t`, rows side by side."""
+    return _torch.empty_like(t) if t.is_contiguous() else t.new_empty(t.shape)
 
 
 def _ptr(t):
@@ -96,58 +112,73 @@ def _ptr(t):
 def tm_layer_norm(x, weight=None, bias=None, eps: float = 1e-5, residual=None, y=None, sum_out=None, mean_out=None, rstd_out=None,
                   want_sum: bool = True, want_stats: bool = True, stream=None):
     """Layer norm of x, or of x + residual, over the columns.  Returns (y, x + residual or None, mean, rstd)."""
-    import torch
-    dev = x.device
-    code, ld = _code(x, "x"), _matrix(x, "x")
-    rows, cols = x.shape
+    lib = _lib()
+    code, dev, rows, cols, ld = _input(x, "x")
     _, wcode, wp, bp = _params(weight, bias, cols, dev, x.dtype)
-    ld_r = _matrix(residual, "residual", x) if residual is not None else cols
+    ld_r = ld_s = ld_y = cols
     if residual is None:
         sum_out = None
-    elif sum_out is None and want_sum:
-        sum_out = torch.empty((rows, cols), dtype=x.dtype, device=dev)
-    if y is None:
-        y = torch.empty((rows, cols), dtype=x.dtype, device=dev)
-    if want_stats:
-        if mean_out is None:
-            mean_out = torch.empty((rows,), dtype=torch.float32, device=dev)
-        if rstd_out is None:
-            rstd_out = torch.empty((rows,), dtype=torch.float32, device=dev)
-    ld_s = _matrix(sum_out, "sum_out", x) if sum_out is not None else cols
-    _call(_lib().tm_layer_norm, dev, stream, x.data_ptr(), ld, _ptr(residual), ld_r, code, rows, cols, wp, bp, wcode, eps, _ptr(sum_out), ld_s,
-          y.data_ptr(), _matrix(y, "y", x), _array(mean_out, (rows,), torch.float32, dev, "mean_out"), _array(rstd_out, (rows,), torch.float32, dev, "rstd_out"))
+    else:
+        ld_r = _other(residual, "residual", x)
+        if sum_out is not None:
+            ld_s = _other(sum_out, "sum_out", x)
+        elif want_sum:
+            sum_out = _like(x)
+    if y is not None:
+        ld_y = _other(y, "y", x)
+    else:
+        y = _like(x)
+    mp = rp = None
+    f32 = _torch.float32
+    if want_stats and mean_out is None and rstd_out is None:
+        mean_out, rstd_out = _torch.empty((2, rows), dtype=f32, device=dev).unbind(0)
+        mp, rp = mean_out.data_ptr(), rstd_out.data_ptr()
+    else:
+        if want_stats:
+            mean_out = _torch.empty((rows,), dtype=f32, device=dev) if mean_out is None else mean_out
+            rstd_out = _torch.empty((rows,), dtype=f32, device=dev) if rstd_out is None else rstd_out
+        mp, rp = _array(mean_out, (rows,), f32, dev, "mean_out"), _array(rstd_out, (rows,), f32, dev, "rstd_out")
+    _call(lib.tm_layer_norm, dev, stream, x.data_ptr(), ld, _ptr(residual), ld_r, code, rows, cols, wp, bp, wcode, eps, _ptr(sum_out), ld_s,
+          y.data_ptr(), ld_y, mp, rp)
     return y, sum_out, mean_out, rstd_out
 
 
 def tm_layer_norm_workspace_bytes(rows: int, cols: int) -> int:
-    return int(_lib().tm_layer_norm_workspace_bytes(rows, cols))
+    return _lib().tm_layer_norm_workspace_bytes(rows, cols)
 
 
 def tm_layer_norm_backward(dy, h, mean, rstd, weight=None, dsum=None, dx=None, dweight_out=None, dbias_out=None, workspace=None,
                            want_params: bool = True, params_dtype=None, stream=None):
     """Gradients of the layer norm of h (x, or the sum that tm_layer_norm returned).  Returns (dx, dweight, dbias); the last two have
     the weight's dtype (without a weight `params_dtype`, or h's), and are None with want_params=False."""
-    import torch
-    dev = h.device
-    code, ld_h = _code(h, "h"), _matrix(h, "h")
-    rows, cols = h.shape
+    lib = _lib()
+    code, dev, rows, cols, ld_h = _input(h, "h")
     kind, wcode, wp, _ = _params(weight, None, cols, dev, params_dtype or h.dtype)
-    if dx is None:
-        dx = torch.empty((rows, cols), dtype=h.dtype, device=dev)
-    bytes_ = 0
-    if want_params:
-        if dweight_out is None:
-            dweight_out = torch.empty((cols,), dtype=kind, device=dev)
-        if dbias_out is None:
-            dbias_out = torch.empty((cols,), dtype=kind, device=dev)
+    ld_dy, ld_s, ld_dx, f32 = _other(dy, "dy", h), cols, cols, _torch.float32
+    if dsum is not None:
+        ld_s = _other(dsum, "dsum", h)
+    if dx is not None:
+        ld_dx = _other(dx, "dx", h)
+    else:
+        dx = _like(h)
+    wsp, bytes_, dwp, dbp = None, 0, None, None
+    if want_params and dweight_out is None and dbias_out is None:
+        dweight_out, dbias_out = _torch.empty((2, cols), dtype=kind, device=dev).unbind(0)
+        dwp, dbp = dweight_out.data_ptr(), dbias_out.data_ptr()
+    else:
+        if want_params:
+            dweight_out = _torch.empty((cols,), dtype=kind, device=dev) if dweight_out is None else dweight_out
+            dbias_out = _torch.empty((cols,), dtype=kind, device=dev) if dbias_out is None else dbias_out
+        dwp, dbp = _array(dweight_out, (cols,), kind, dev, "dweight_out"), _array(dbias_out, (cols,), kind, dev, "dbias_out")
     if dweight_out is not None or dbias_out is not None:
         if workspace is None:
-            workspace = torch.empty((tm_layer_norm_workspace_bytes(rows, cols),), dtype=torch.uint8, device=dev)
-        bytes_ = workspace.numel() * workspace.element_size()
-    _call(_lib().tm_layer_norm_backward, dev, stream, dy.data_ptr(), _matrix(dy, "dy", h), h.data_ptr(), ld_h, code, rows, cols, wp, wcode,
-          _array(mean, (rows,), torch.float32, dev, "mean"), _array(rstd, (rows,), torch.float32, dev, "rstd"),
-          _ptr(dsum), _matrix(dsum, "dsum", h) if dsum is not None else cols, dx.data_ptr(), _matrix(dx, "dx", h),
-          _array(dweight_out, (cols,), kind, dev, "dweight_out"), _array(dbias_out, (cols,), kind, dev, "dbias_out"), _ptr(workspace), bytes_)
+            bytes_ = lib.tm_layer_norm_workspace_bytes(rows, cols)
+            workspace = _torch.empty((bytes_,), dtype=_torch.uint8, device=dev)
+        else:
+            bytes_ = workspace.numel() * workspace.element_size()
+        wsp = workspace.data_ptr()
+    _call(lib.tm_layer_norm_backward, dev, stream, dy.data_ptr(), ld_dy, h.data_ptr(), ld_h, code, rows, cols, wp, wcode,
+          _array(mean, (rows,), f32, dev, "mean"), _array(rstd, (rows,), f32, dev, "rstd"), _ptr(dsum), ld_s, dx.data_ptr(), ld_dx, dwp, dbp, wsp, bytes_)
     return dx, dweight_out, dbias_out
 
 
@@ -155,71 +186,72 @@ def tm_top_logits(logits, k: int, temperature: float = 1.0, values_out=None, ids
                   status=None, stream=None):
     """The k largest logits of every row (equal ones by the lower id) and log sum exp(logits / temperature).
     Returns (values float32 [rows, k], ids int32 [rows, k], lse float32 [rows] or None).  status: int32[1] or None."""
-    import torch
-    dev = logits.device
-    code, ld = _code(logits, "logits"), _matrix(logits, "logits")
-    rows, vocab = logits.shape
+    lib = _lib()
+    code, dev, rows, vocab, ld = _input(logits, "logits")
+    f32, i32, shape = _torch.float32, _torch.int32, (rows, max(k, 0))
     if values_out is None:
-        values_out = torch.empty((rows, max(k, 0)), dtype=torch.float32, device=dev)
+        values_out = _torch.empty(shape, dtype=f32, device=dev)
     if ids_out is None:
-        ids_out = torch.empty((rows, max(k, 0)), dtype=torch.int32, device=dev)
+        ids_out = _torch.empty(shape, dtype=i32, device=dev)
     if lse_out is None and want_lse:
-        lse_out = torch.empty((rows,), dtype=torch.float32, device=dev)
-    _call(_lib().tm_top_logits, dev, stream, logits.data_ptr(), code, rows, vocab, ld, k, temperature,
-          _array(values_out, (rows, k), torch.float32, dev, "values_out"), _array(ids_out, (rows, k), torch.int32, dev, "ids_out"),
-          _array(lse_out, (rows,), torch.float32, dev, "lse_out"), _array(status, (1,), torch.int32, dev, "status"))
+        lse_out = _torch.empty((rows,), dtype=f32, device=dev)
+    _call(lib.tm_top_logits, dev, stream, logits.data_ptr(), code, rows, vocab, ld, k, temperature, _array(values_out, shape, f32, dev, "values_out"),
+          _array(ids_out, shape, i32, dev, "ids_out"), _array(lse_out, (rows,), f32, dev, "lse_out"), _array(status, (1,), i32, dev, "status"))
     return values_out, ids_out, lse_out
 
 
 def _lists(logits, top_values, top_ids, teacher_lse, row_weight, temperature, scale):
-    import torch
-    dev = logits.device
-    code, ld = _code(logits, "logits"), _matrix(logits, "logits")
-    rows, vocab = logits.shape
+    code, dev, rows, vocab, ld = _input(logits, "logits")
     if top_ids.dim() != 2:
         raise TmError(2, "top_ids must be [rows, k]")
-    k = top_ids.shape[1]
-    return dev, rows, vocab, (logits.data_ptr(), code, rows, vocab, ld, _array(top_values, (rows, k), torch.float32, dev, "top_values"),
-                              _array(top_ids, (rows, k), torch.int32, dev, "top_ids"), k, _array(teacher_lse, (rows,), torch.float32, dev, "teacher_lse"),
-                              _array(row_weight, (rows,), torch.float32, dev, "row_weight"), temperature, scale)
+    k, f32 = top_ids.shape[1], _torch.float32
+    return dev, rows, (logits.data_ptr(), code, rows, vocab, ld, _array(top_values, (rows, k), f32, dev, "top_values"),
+                       _array(top_ids, (rows, k), _torch.int32, dev, "top_ids"), k, _array(teacher_lse, (rows,), f32, dev, "teacher_lse"),
+                       _array(row_weight, (rows,), f32, dev, "row_weight"), temperature, scale)
 
 
 def tm_distill_loss(logits, top_values, top_ids, teacher_lse=None, row_weight=None, temperature: float = 1.0, scale: float = 1.0,
                     loss_out=None, stats_out=None, want_stats: bool = True, status=None, stream=None):
     """Loss of every row (float32 [rows]) and the statistics [rows, 2] that tm_distill_grad takes."""
-    import torch
-    dev, rows, _, head = _lists(logits, top_values, top_ids, teacher_lse, row_weight, temperature, scale)
+    lib = _lib()
+    dev, rows, head = _lists(logits, top_values, top_ids, teacher_lse, row_weight, temperature, scale)
+    f32 = _torch.float32
     if loss_out is None:
-        loss_out = torch.empty((rows,), dtype=torch.float32, device=dev)
+        loss_out = _torch.empty((rows,), dtype=f32, device=dev)
     if stats_out is None and want_stats:
-        stats_out = torch.empty((rows, 2), dtype=torch.float32, device=dev)
-    _call(_lib().tm_distill_loss, dev, stream, *head, _array(loss_out, (rows,), torch.float32, dev, "loss_out"),
-          _array(stats_out, (rows, 2), torch.float32, dev, "stats_out"), _array(status, (1,), torch.int32, dev, "status"))
+        stats_out = _torch.empty((rows, 2), dtype=f32, device=dev)
+    _call(lib.tm_distill_loss, dev, stream, *head, _array(loss_out, (rows,), f32, dev, "loss_out"),
+          _array(stats_out, (rows, 2), f32, dev, "stats_out"), _array(status, (1,), _torch.int32, dev, "status"))
     return loss_out, stats_out
 
 
 def tm_distill_grad(logits, top_values, top_ids, stats, grad_loss=None, teacher_lse=None, row_weight=None, temperature: float = 1.0,
                     scale: float = 1.0, dlogits=None, status=None, stream=None):
     """Gradient of the logits from the statistics of tm_distill_loss, times grad_loss[row] where given."""
-    import torch
-    dev, rows, vocab, head = _lists(logits, top_values, top_ids, teacher_lse, row_weight, temperature, scale)
-    if dlogits is None:
-        dlogits = torch.empty((rows, vocab), dtype=logits.dtype, device=dev)
-    _call(_lib().tm_distill_grad, dev, stream, *head, _array(stats, (rows, 2), torch.float32, dev, "stats"),
-          _array(grad_loss, (rows,), torch.float32, dev, "grad_loss"), dlogits.data_ptr(), _matrix(dlogits, "dlogits", logits),
-          _array(status, (1,), torch.int32, dev, "status"))
+    lib = _lib()
+    dev, rows, head = _lists(logits, top_values, top_ids, teacher_lse, row_weight, temperature, scale)
+    f32, ld_d = _torch.float32, logits.shape[1]
+    if dlogits is not None:
+        ld_d = _other(dlogits, "dlogits", logits)
+    else:
+        dlogits = _like(logits)
+    _call(lib.tm_distill_grad, dev, stream, *head, _array(stats, (rows, 2), f32, dev, "stats"), _array(grad_loss, (rows,), f32, dev, "grad_loss"),
+          dlogits.data_ptr(), ld_d, _array(status, (1,), _torch.int32, dev, "status"))
     return dlogits
 
 
 def tm_distill_loss_grad(logits, top_values, top_ids, teacher_lse=None, row_weight=None, temperature: float = 1.0, scale: float = 1.0,
                          loss_out=None, dlogits=None, status=None, stream=None):
     """Loss of every row and the gradient of their sum, in one pass over the logits.  Returns (loss [rows], dlogits)."""
-    import torch
-    dev, rows, vocab, head = _lists(logits, top_values, top_ids, teacher_lse, row_weight, temperature, scale)
+    lib = _lib()
+    dev, rows, head = _lists(logits, top_values, top_ids, teacher_lse, row_weight, temperature, scale)
+    ld_d = logits.shape[1]
     if loss_out is None:
-        loss_out = torch.empty((rows,), dtype=torch.float32, device=dev)
-    if dlogits is None:
-        dlogits = torch.empty((rows, vocab), dtype=logits.dtype, device=dev)
-    _call(_lib().tm_distill_loss_grad, dev, stream, *head, _array(loss_out, (rows,), torch.float32, dev, "loss_out"),
-          dlogits.data_ptr(), _matrix(dlogits, "dlogits", logits), _array(status, (1,), torch.int32, dev, "status"))
+        loss_out = _torch.empty((rows,), dtype=_torch.float32, device=dev)
+    if dlogits is not None:
+        ld_d = _other(dlogits, "dlogits", logits)
+    else:
+        dlogits = _like(logits)
+    _call(lib.tm_distill_loss_grad, dev, stream, *head, _array(loss_out, (rows,), _torch.float32, dev, "loss_out"), dlogits.data_ptr(), ld_d,
+          _array(status, (1,), _torch.int32, dev, "status"))
     return loss_out, dlogits

@@ -27,7 +27,7 @@ struct Lists {
 
 int check_distill(const void* logits, int dtype, int64_t rows, int64_t vocab, int64_t ld, const Lists& l, const int* status) {
     if (!good_dtype(dtype)) return TM_ERR_DTYPE;
-    if (!good_rows(rows, vocab) || !good_ld(rows, vocab, ld) || vocab > INT32_MAX) return TM_ERR_SHAPE;
+    if (!good_rows(rows, vocab) || !good_ld(rows, vocab, ld) || vocab > TM_VOCAB_MAX) return TM_ERR_SHAPE;
     if (l.k < 0 || l.k > TM_TOP_MAX || !(l.temperature > 0.0f) || !std::isfinite(l.temperature) || !std::isfinite(l.scale)) return TM_ERR_RANGE;
     if (rows == 0) return TM_OK;
     if ((vocab > 0 && !logits) || (l.k > 0 && (!l.values || !l.ids))) return TM_ERR_NULL;
@@ -105,7 +105,7 @@ int tm_layer_norm_backward(const void* dy, int64_t ld_dy, const void* h, int64_t
 int tm_top_logits(const void* logits, int dtype, int64_t rows, int64_t vocab, int64_t ld, int k, float temperature,
                   float* values_out, int32_t* ids_out, float* lse_out, int* status_dev, void* cuda_stream) {
     if (!good_dtype(dtype)) return TM_ERR_DTYPE;
-    if (!good_rows(rows, vocab) || !good_ld(rows, vocab, ld) || vocab > INT32_MAX) return TM_ERR_SHAPE;
+    if (!good_rows(rows, vocab) || !good_ld(rows, vocab, ld) || vocab > TM_VOCAB_MAX) return TM_ERR_SHAPE;
     if (k < 1 || k > TM_TOP_MAX || !(temperature > 0.0f) || !std::isfinite(temperature)) return TM_ERR_RANGE;
     if (rows == 0) return TM_OK;
     if ((vocab > 0 && !logits) || !values_out || !ids_out) return TM_ERR_NULL;

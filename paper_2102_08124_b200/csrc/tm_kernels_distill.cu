@@ -19,13 +19,6 @@ namespace {
 
 constexpr double kLog2eD = 1.4426950408889634074, kLn2D = 0.69314718055994530942;
 
-// A row's list as the kernels use it: entries in their order, unusable ones (padding, out of range, repeated) with id -1.
-struct List {
-    int id[kTopMax];
-    float p[kTopMax];      // the teacher's probability of the entry
-    float z[kTopMax];      // the student's logit
-};
-
 __device__ __forceinline__ float warp_sum(float v) { return group_sum<32>(v); }
 __device__ __forceinline__ double warp_sum_double(double v) {
 #pragma unroll
@@ -33,182 +26,592 @@ __device__ __forceinline__ double warp_sum_double(double v) {
     return v;
 }
 
-// Any vocabulary: one CTA a row.  Which logits are listed is asked of a bit filter over id mod 32768 first and of the list
-// itself only where the filter says so.
-constexpr int kWideThreads = 512, kFilterBits = 32768;
-template <int DT, bool LOSS, bool GRAD> __global__ void __launch_bounds__(kWideThreads) wide_distill_kernel(const DistillArgs a) {
-    constexpr int V = RowType<DT>::kVec, kWarps = kWideThreads / 32;
-    __shared__ List list;
-    __shared__ uint32_t filter[kFilterBits / 32];
-    __shared__ float bm[kWarps], bs[kWarps];
-    __shared__ double bd[kWarps];
-    __shared__ float share[8];
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const float inv_t = 1.0f / a.temperature, c2 = (float)(kLog2eD / a.temperature);
+constexpr int kHash = 512, kEntries = kTopMax / 32;      // slots of the table that finds repeated ids; entries of a lane
+
+__device__ __forceinline__ float lowest() { return -3.4028234663852886e38f; }
+
+// 2^(x - R) of a logit: `slow` rows (R outside the range in which x = z c2 is safe) have R in logits and take the difference first.
+// LOSS: R from the row's own sums; otherwise from the statistics, a log-sum-exp in units of the temperature.
+template <bool LOSS> __device__ __forceinline__ float power_of(float z, float R, bool slow, float c2, float inv_t) {
+    if (!slow) return exp2_fast(fmaf(z, c2, -R));
+    return LOSS ? exp2_fast((z - R) * c2) : exp2_fast(fmaf(z, inv_t, -R) * (float)kLog2eD);
+}
+
+// What a row's gradient needs beside its list: q = 2^(x - R) inv, unlisted logits times off.
+struct Scale { float R, inv, off; bool slow; };
+__device__ __forceinline__ Scale scale_of_stats(float lse, float log_rest, float rest) {
+    // q = 2^(x - R) 2^(R - lse log2 e): the second factor, of R's rounding, joins the others
+    const double want = (double)lse * kLog2eD;
+    Scale k;
+    k.R = (float)want;
+    k.slow = !(fabsf(k.R) < 1e30f);
+    k.inv = k.slow ? 1.0f : exp2f((float)((double)k.R - want));
+    if (k.slow) k.R = lse;
+    k.off = rest > 0.0f && log_rest > -INFINITY ? 1.0f - rest * expf(-log_rest) : 1.0f;
+    return k;
+}
+
+// A row's list, entry e * 32 + lane in the lanes of one warp: unusable entries (padding, out of range, repeated) get id -1.
+struct List {
+    int id[kEntries];
+    float p[kEntries];     // the teacher's probability (its logit until probabilities() ran)
+    float entropy, mass;   // sum p (log p + log norm), sum p
+    float norm;            // what the exponentials were divided by (1 where the teacher's log-sum-exp is given)
+    float rest;            // p_rest
+    bool some;             // any entry
+
+    // between rows and barriers a list waits in shared memory: ids and values, kTopMax each
+    __device__ __forceinline__ void load(const int* ids, const float* values, int slots) {
+        const int lane = threadIdx.x & 31;
+#pragma unroll
+        for (int e = 0; e < kEntries; ++e) {
+            id[e] = -1; p[e] = 0.0f;
+            if (e * 32 < slots) { id[e] = ids[e * 32 + lane]; p[e] = values[e * 32 + lane]; }
+        }
+    }
+    // true if an entry was out of range or repeated.  `hash`: kHash words of -1 (left so), this warp's own.
+    __device__ __forceinline__ bool weed(const DistillArgs& a, int slots, int* hash) {
+        const int lane = threadIdx.x & 31;
+        bool bad = false, again = false;
+        int at[kEntries];
+#pragma unroll
+        for (int e = 0; e < kEntries; ++e)
+            if (id[e] >= a.vocab) { id[e] = -1; bad = true; }
+        // the table tells whether ids repeat at all; only then the first of each is looked for
+#pragma unroll
+        for (int e = 0; e < kEntries; ++e) {
+            at[e] = -1;
+            if (e * 32 < slots && id[e] >= 0) {
+                int h = (int)(((uint32_t)id[e] * 2654435769u) >> 23);
+                for (int probe = 0; probe < kHash; ++probe) {
+                    const int old = atomicCAS(&hash[h], -1, id[e]);
+                    if (old == -1) { at[e] = h; break; }
+                    if (old == id[e]) { again = true; break; }
+                    h = (h + 1) & (kHash - 1);
+                }
+            }
+        }
+        __syncwarp();
+#pragma unroll
+        for (int e = 0; e < kEntries; ++e)
+            if (at[e] >= 0) hash[at[e]] = -1;
+        __syncwarp();
+        if (__any_sync(0xFFFFFFFFu, again)) {
+            int gone = 0;                                 // bit e: an earlier entry has this id
+#pragma unroll
+            for (int j = 0; j < kEntries; ++j) {
+                if (j * 32 >= slots) break;
+                for (int l = 0; l < 32; ++l) {
+                    const int other = __shfl_sync(0xFFFFFFFFu, id[j], l);
+#pragma unroll
+                    for (int e = 0; e < kEntries; ++e)
+                        if (id[e] == other && j * 32 + l < e * 32 + lane) gone |= 1 << e;
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < kEntries; ++e)
+                if (gone >> e & 1) id[e] = -1;
+        }
+        return bad | again;
+    }
+    // log p = (v - top) / T - log norm, or v / T - lse with one rounding of the difference (1 / T = it + it_low)
+    __device__ __forceinline__ void probabilities(const DistillArgs& a, float weight, float lse_t, float it, float it_low) {
+        float top = -INFINITY;
+        some = false;
+        entropy = mass = rest = 0.0f;
+        norm = 1.0f;
+#pragma unroll
+        for (int e = 0; e < kEntries; ++e)
+            if (id[e] >= 0) { some = true; top = fmaxf(top, p[e]); }
+        some = __any_sync(0xFFFFFFFFu, some) && weight != 0.0f;
+        if (!some) return;
+        float log_p[kEntries];
+        const bool own = !a.teacher_lse;
+        if (own) top = group_max<32>(top);
+#pragma unroll
+        for (int e = 0; e < kEntries; ++e) {
+            log_p[e] = 0.0f;
+            if (id[e] >= 0) {
+                log_p[e] = own ? (p[e] - top) * it : fmaf(p[e], it, -lse_t) + (p[e] > -INFINITY ? p[e] * it_low : 0.0f);
+                p[e] = expf(log_p[e]);
+            } else p[e] = 0.0f;
+            mass += p[e];
+        }
+        mass = group_sum<32>(mass);
+        float scale = 1.0f;
+        if (own) {
+            norm = mass;
+            scale = 1.0f / norm;
+            mass = 1.0f;
+        } else rest = fmaxf(0.0f, 1.0f - mass);
+#pragma unroll
+        for (int e = 0; e < kEntries; ++e) {
+            p[e] *= scale;
+            if (p[e] != 0.0f) entropy = fmaf(p[e], log_p[e], entropy);
+        }
+        entropy = group_sum<32>(entropy);
+    }
+};
+
+// One warp: row r's list as given into shared memory (entries past it as padding).
+__device__ __forceinline__ void fetch_list(const DistillArgs& a, long long r, int slots, int* ids, float* values) {
+    for (int k = threadIdx.x & 31; k < slots; k += 32) {
+        const bool in = k < a.k;
+        ids[k] = in ? a.ids[r * a.k + k] : -1;
+        values[k] = in ? a.values[r * a.k + k] : 0.0f;
+    }
+    __syncwarp();
+}
+
+// A row's loss, by one warp: sum p log p - sum p log q + p_rest (log p_rest - log q_rest), put together in 64 bits because the sums
+// nearly cancel.  The four logs are taken side by side in four lanes.  dot: sum p z; lse_shift: what the exponentials' sums are
+// relative to, in units of the temperature.  Lane 0 returns the loss, and the statistics.
+__device__ __forceinline__ float row_loss(float entropy, float mass, float norm, float rest, double dot, double inv_t, double lse_shift, float s_all, float s_rest,
+                                          float& lse, float& log_rest) {
+    const int lane = threadIdx.x & 31;
+    const double l = log((double)(lane == 0 ? s_all : lane == 1 ? s_rest : lane == 2 ? rest : norm));
+    const double log_s = __shfl_sync(0xFFFFFFFFu, l, 1), log_r = __shfl_sync(0xFFFFFFFFu, l, 2), log_n = __shfl_sync(0xFFFFFFFFu, l, 3);
+    const double lse_d = lse_shift + l, log_rest_d = log_s - l;          // lane 0's
+    double loss = (double)entropy - mass * log_n - dot * inv_t + mass * lse_d;
+    if (rest > 0.0f && s_rest > 0.0f) loss += rest * (log_r - log_rest_d);
+    if (s_rest != s_rest) loss = s_rest;
+    lse = (float)lse_d;
+    log_rest = (float)log_rest_d;
+    return (float)loss;
+}
+
+// ---- a row by a cluster of thread blocks -----------------------------------------------------------------------------
+//
+// Bound: HBM, with the exponentials close behind (a logit costs one in the loss and one in the gradient; the units that make them
+// give 16 a clock and SM).  C blocks share a row, a slice each: NT workers and one warp for the list.
+//   pass 1  the workers' running maximum and sum over their vectors of the slice; meanwhile the list's warp works out the teacher's
+//           probabilities and the listed logits' part.  Listed logits stay out of the workers' sum by a byte of flags for every
+//           vector in shared memory, which is zero nearly always.
+//   totals  the warps' partial results, by shared memory (of the whole cluster)
+//   pass 2  the gradient, from the copy of the slice that pass 1 left in shared memory: a row is read once.  Meanwhile the list's
+//           warp puts the loss together; after the pass it writes the listed logits' gradients.
+// Several blocks share an SM, so one's loads cover another's exponentials and waits.
+// Exponents live in base 2, scaled: x_j = z_j c2 with c2 = log2(e) / T, as differences x_j - R with one rounding (fma), R the largest
+// x.  A row whose R lies outside +-1e30 (all logits masked by the type's lowest value, say) goes again with the difference first.
+
+constexpr int kMaxCluster = 8;
+constexpr size_t kRowSmem = 216 * 1024;            // of a block's 227 KB, beside the static arrays
+
+struct RowPlan {
+    int cluster, slots;            // slots: list entries, a multiple of 32
+    int slice_vectors, flags;      // flags: bytes, a multiple of 16 (0 without a loss)
+    int stash;                     // blocks of NT * U vectors that stay in shared memory between the passes
+    double kappa;                  // (log2(e) / T) / c2, the rounding of c2
+};
+
+constexpr int kBlockVectors = 4;                   // vectors of a thread's block
+template <int NT> constexpr int kBlocks = NT >= 384 ? 2 : NT == 256 ? 3 : 6;   // blocks an SM: the registers they may use
+
+template <int DT, bool LOSS, bool GRAD, int NT>
+__global__ void __launch_bounds__(NT + 32, kBlocks<NT>) distill_kernel(const DistillArgs a, const RowPlan plan) {
     using T = typename RowType<DT>::T;
-    for (long long r = blockIdx.x; r < a.rows; r += gridDim.x) {
+    constexpr int V = RowType<DT>::kVec, NW = NT / 32, U = kBlockVectors;
+    extern __shared__ __align__(16) uint8_t dynamic[];
+    uint8_t* const flags = dynamic;
+    uint4* const stash = reinterpret_cast<uint4*>(dynamic + plan.flags);
+    __shared__ int hash[kHash];
+    __shared__ int list_id[kTopMax];                                      // the row's list as given, then without what was weeded out
+    __shared__ float list_v[kTopMax];
+    __shared__ int list_at[kTopMax];                                      // ids of this slice's listed logits, or -1
+    __shared__ float list_p[kTopMax], list_z[kTopMax];
+    __shared__ float2 part[2][NW], list_part[2];
+    __shared__ double dot_part[2];
+    __shared__ float rest_s;
+    __shared__ int on_s;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const bool lister = warp == NW;
+    const int C = plan.cluster, slots = plan.slots;
+    const uint32_t rank = C > 1 ? cluster_rank() : 0u;
+    const float inv_t = 1.0f / a.temperature, c2 = (float)(kLog2eD / a.temperature);
+    const long long step = gridDim.x / C;
+    for (int i = tid; i < kHash; i += NT + 32) hash[i] = -1;
+    for (int i = tid; i < plan.flags / 16; i += NT + 32) reinterpret_cast<uint4*>(flags)[i] = make_uint4(0u, 0u, 0u, 0u);
+    int turn = 0;
+    float next_weight = 1.0f;                                             // read a row ahead, as is the list
+    uint4 even[U], odd[U];
+    const long long start = blockIdx.x / C;
+    if (start < a.rows) {
+        if (a.row_weight) next_weight = a.row_weight[start];
+        if (lister) fetch_list(a, start, slots, list_id, list_v);
+    }
+    __syncthreads();
+
+    for (long long r = start; r < a.rows; r += step) {
         const RowVectors<DT> row(static_cast<const T*>(a.logits) + r * a.ld, a.vocab);
-        T* out = GRAD ? static_cast<T*>(a.dlogits) + r * a.ld_d : nullptr;
-        const bool same = GRAD && ((reinterpret_cast<uintptr_t>(out) ^ reinterpret_cast<uintptr_t>(row.base)) & 15) == 0;
-        const float weight = a.row_weight ? a.row_weight[r] : 1.0f;
-        for (int i = tid; i < kFilterBits / 32; i += kWideThreads) filter[i] = 0;
-        __syncthreads();
-        // the list: entries in range, the first of equal ids, their logits
-        bool bad = false;
-        if (weight != 0.0f)
-            for (int k = tid; k < a.k; k += kWideThreads) {
-                const int id = a.ids[r * a.k + k];
-                bool ok = id >= 0;
-                if (ok && id >= a.vocab) { ok = false; bad = true; }
-                for (int j = 0; ok && j < k; ++j)
-                    if (a.ids[r * a.k + j] == id) { ok = false; bad = true; }
-                list.id[k] = ok ? id : -1;
-                list.z[k] = ok ? to_float(row.base[id]) : 0.0f;
-                if (ok) atomicOr(&filter[(id & (kFilterBits - 1)) >> 5], 1u << (id & 31));
-            }
-        if (bad && a.status) atomicOr(a.status, kDevBadId);
-        __syncthreads();
-        // the teacher's side, by one warp
-        if (warp == 0) {
-            float vm = -INFINITY;
-            int n = 0;
-            if (weight != 0.0f)
-                for (int k = lane; k < a.k; k += 32)
-                    if (list.id[k] >= 0) { vm = fmaxf(vm, a.values[r * a.k + k] * inv_t); ++n; }
-            vm = group_max<32>(vm);
-            n = (int)__reduce_add_sync(0xFFFFFFFFu, (unsigned)n);
-            float shift = a.teacher_lse ? a.teacher_lse[r] : 0.0f, s = 0.0f;
-            if (!a.teacher_lse) {
-                if (n > 0)
-                    for (int k = lane; k < a.k; k += 32)
-                        if (list.id[k] >= 0) s += expf(a.values[r * a.k + k] * inv_t - vm);
-                s = warp_sum(s);
-                shift = vm + logf(s);
-            }
-            double mass = 0.0, ent = 0.0;
-            for (int k = lane; n > 0 && k < a.k; k += 32)
-                if (list.id[k] >= 0) {
-                    const float lp = a.values[r * a.k + k] * inv_t - shift, p = expf(lp);
-                    list.p[k] = p;
-                    mass += p;
-                    if (p != 0.0f) ent += (double)p * lp;
+        const long long from = min(row.count, (long long)rank * plan.slice_vectors), to = min(row.count, from + plan.slice_vectors);
+        const RowPart<DT> slice(row, from, to);
+        const uint4* const vec = reinterpret_cast<const uint4*>(row.base + slice.column);
+        const int inside = slice.inside, edges = slice.head + slice.tail;
+        T* const out = GRAD ? static_cast<T*>(a.dlogits) + r * a.ld_d : nullptr;
+        const float weight = next_weight;
+        if (a.row_weight && r + step < a.rows) next_weight = a.row_weight[r + step];
+        // A thread's vectors come in blocks of U, NT apart; all blocks but the last are whole.  Two register blocks take turns, so that
+        // one is on its way while the other is worked on; the first is on its way while the list is read.
+        const int whole = inside / (NT * U), blocks = (inside + NT * U - 1) / (NT * U);
+        auto fetch = [&](uint4 (&w)[U], const uint4* src, int b) {
+            src += b * (NT * U) + tid;
+            if (b < whole) {
+#pragma unroll
+                for (int u = 0; u < U; ++u) w[u] = src[u * NT];
+            } else {
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    w[u] = make_uint4(RowType<DT>::kLow, RowType<DT>::kLow, RowType<DT>::kLow, RowType<DT>::kLow);
+                    if (b * (NT * U) + u * NT + tid < inside) w[u] = src[u * NT];
                 }
-            mass = warp_sum_double(mass);
-            ent = warp_sum_double(ent);
-            if (lane == 0) {
-                const float rest = a.teacher_lse ? fmaxf(0.0f, (float)(1.0 - mass)) : 0.0f;
-                share[0] = __int_as_float(n);
-                share[1] = rest;
-                bd[0] = ent; bd[1] = mass;
             }
-        }
-        __syncthreads();
-        const bool on = weight != 0.0f && __float_as_int(share[0]) > 0;
-        const float rest = share[1];
-        const double entropy = bd[0], mass = bd[1];
-        __syncthreads();
-        if (!on) {
-            if (tid == 0) {
-                if (LOSS) a.loss[r] = 0.0f;
-                if (LOSS && a.stats) a.stats[2 * r] = a.stats[2 * r + 1] = 0.0f;
-            }
-            if constexpr (GRAD) {
-                const float zero[V] = {};
-                for (long long i = tid; i < row.count; i += kWideThreads) row.store(out, same, i, zero);
-            }
-            continue;
-        }
-        auto listed = [&](long long c) {
-            if (!((filter[(c & (kFilterBits - 1)) >> 5] >> (c & 31)) & 1u)) return -1;
-            for (int k = 0; k < a.k; ++k)
-                if (list.id[k] == c) return k;
-            return -1;
         };
-        // q_j = 2^((z_j - ref) c2 - shift2): the difference first, so that a row of the type's lowest numbers keeps its proportions
-        float ref, shift2, log_rest2;                     // log_rest2: log2 of q_rest
-        if constexpr (LOSS) {
-            float m = -INFINITY, s = 0.0f;                // unlisted logits
-            for (long long i = tid; i < row.count; i += kWideThreads) {
-                float v[V];
-                row.load(i, v, -INFINITY);
-                const long long c = row.column(i);
-                float top = m;
-#pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    if (c + j >= 0 && c + j < a.vocab && listed(c + j) >= 0) v[j] = -INFINITY;
-                    top = fmaxf(top, v[j]);
-                }
-                const float ref = top == -INFINITY ? 0.0f : top;
-                s *= exp2_fast((m - ref) * c2);
-#pragma unroll
-                for (int j = 0; j < V; ++j) s += exp2_fast((v[j] - ref) * c2);
-                m = top;
+        // use(block, its number) for all of this thread's blocks, the first `kept` of them from the stash; block 0 is in `even`
+        auto walk = [&](int kept, auto&& use) {
+            for (int b = 0; b < blocks;) {
+                if (b + 1 < blocks) fetch(odd, b + 1 < kept ? stash : vec, b + 1);
+                use(even, b);
+                if (++b == blocks) break;
+                if (b + 1 < blocks) fetch(even, b + 1 < kept ? stash : vec, b + 1);
+                use(odd, b);
+                ++b;
             }
-            float lm = -INFINITY;
-            double dot = 0.0;
-            for (int k = tid; k < a.k; k += kWideThreads)
-                if (list.id[k] >= 0) {
-                    lm = fmaxf(lm, list.z[k]);
-                    if (list.p[k] != 0.0f) dot += (double)list.p[k] * list.z[k];
-                }
-            const float wm = group_max<32>(fmaxf(m, lm));
-            if (lane == 0) bm[warp] = wm;
-            __syncthreads();
-            float M = -INFINITY;
-            for (int w = 0; w < kWarps; ++w) M = fmaxf(M, bm[w]);
-            s = warp_sum(m == -INFINITY ? s : s * exp2_fast((m - M) * c2));
-            float sl = 0.0f;
-            for (int k = tid; k < a.k; k += kWideThreads)
-                if (list.id[k] >= 0) sl += exp2_fast((list.z[k] - M) * c2);
-            sl = warp_sum(sl);
-            dot = warp_sum_double(dot);
-            __syncthreads();
-            if (lane == 0) { bm[warp] = s; bs[warp] = sl; bd[warp] = dot; }
-            __syncthreads();
-            s = sl = 0.0f; dot = 0.0;
-            for (int w = 0; w < kWarps; ++w) { s += bm[w]; sl += bs[w]; dot += bd[w]; }
-            const float all2 = log2f(s + sl);
-            ref = M;
-            shift2 = all2;
-            log_rest2 = log2f(s) - all2;
-            if (tid == 0) {
-                const double lse = (double)M / a.temperature + all2 * kLn2D, log_rest = (double)log_rest2 * kLn2D;
-                double loss = entropy - dot / a.temperature + mass * lse;
-                if (rest > 0.0f && s > 0.0f) loss += (double)rest * (logf(rest) - log_rest);
-                if (s != s) loss = s;
-                a.loss[r] = (float)(loss * weight * a.scale);
-                if (a.stats) { a.stats[2 * r] = (float)lse; a.stats[2 * r + 1] = a.teacher_lse ? (float)log_rest : 0.0f; }
+        };
+        if (lister) {
+            List list;
+            list.load(list_id, list_v, slots);
+            if (list.weed(a, slots, hash) && rank == 0 && weight != 0.0f && a.status) atomicOr(a.status, kDevBadId);
+            bool some = false;
+            const long long c0 = max(0ll, row.column(from)), c1 = row.column(to);
+#pragma unroll
+            for (int e = 0; e < kEntries; ++e) {
+                if (e * 32 >= slots) break;
+                some |= list.id[e] >= 0;
+                const bool here = list.id[e] >= c0 && list.id[e] < c1 && list.id[e] >= 0;
+                list_at[e * 32 + lane] = here ? list.id[e] : -1;
+                if (LOSS) list_id[e * 32 + lane] = list.id[e];
+                const long long place = (long long)list.id[e] - slice.column;             // among the full vectors
+                if (LOSS && here && place >= 0 && place < (long long)inside * V)
+                    atomicOr(reinterpret_cast<uint32_t*>(flags) + (uint32_t)place / (4 * V), 1u << ((uint32_t)place / V % 4 * 8 + (uint32_t)place % V));
+            }
+            some = __any_sync(0xFFFFFFFFu, some) && weight != 0.0f;
+            if (lane == 0) on_s = some;
+            if (!LOSS) {
+                list.probabilities(a, weight, a.teacher_lse ? a.teacher_lse[r] : 0.0f, inv_t, (float)(1.0 / (double)a.temperature - (double)inv_t));
+                if (lane == 0) rest_s = list.rest;
+#pragma unroll
+                for (int e = 0; e < kEntries; ++e)
+                    if (e * 32 < slots) {
+                        const int i = e * 32 + lane;
+                        list_p[i] = list.p[e];
+                        list_z[i] = list_at[i] >= 0 ? to_float(row.base[list_at[i]]) : 0.0f;   // before anything is written: dlogits may be the logits
+                    }
             }
         } else {
-            ref = a.stats[2 * r];
-            shift2 = 0.0f;
-            log_rest2 = (float)(a.stats[2 * r + 1] * kLog2eD);
-        }
-        if constexpr (GRAD) {
-            const float up = weight * a.scale * inv_t * (a.grad_loss ? a.grad_loss[r] : 1.0f);
-            const float off = rest > 0.0f && log_rest2 > -INFINITY ? 1.0f - rest * exp2f(-log_rest2) : 1.0f;
-            for (long long i = tid; i < row.count; i += kWideThreads) {
-                float v[V];
-                row.load(i, v, 0.0f);
-                const long long c = row.column(i);
-#pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    const float q = LOSS ? exp2_fast(fmaf(v[j] - ref, c2, -shift2)) : exp2_fast(fmaf(v[j], inv_t, -ref) * (float)kLog2eD);
-                    const int k = c + j >= 0 && c + j < a.vocab ? listed(c + j) : -1;
-                    v[j] = up * (k >= 0 ? q - list.p[k] : q * off);
-                }
-                row.store(out, same, i, v);
-            }
+            if (weight != 0.0f && blocks > 0) fetch(even, vec, 0);
         }
         __syncthreads();
+        const bool on = on_s;
+        auto unflag = [&](int e) {                        // the lister clears what it set
+            const long long place = (long long)list_at[e] - slice.column;
+            if (list_at[e] >= 0 && place >= 0 && place < (long long)inside * V) reinterpret_cast<uint32_t*>(flags)[(uint32_t)place / (4 * V)] = 0u;
+        };
+        // the gradient's full vectors and edge elements: what(vector or element) as stored
+        const bool same = GRAD && ((reinterpret_cast<uintptr_t>(out) ^ reinterpret_cast<uintptr_t>(row.base)) & 15) == 0;
+        auto put = [&](int i, const uint32_t (&q)[4]) {
+            if (same) __stcs(reinterpret_cast<uint4*>(out + slice.column) + i, make_uint4(q[0], q[1], q[2], q[3]));
+            else {
+                float v[V];
+                unpack_words<DT, 4>(q, v);
+#pragma unroll
+                for (int j = 0; j < V; ++j) from_float(out + slice.column + (long long)i * V + j, v[j]);
+            }
+        };
+        if (!on) {
+            if (LOSS && rank == 0 && tid == 0) {
+                a.loss[r] = 0.0f;
+                if (!GRAD && a.stats) a.stats[2 * r] = a.stats[2 * r + 1] = 0.0f;
+            }
+            if constexpr (GRAD) {
+                const uint32_t zero[4] = {0u, 0u, 0u, 0u};
+                if (!lister) {
+                    for (int i = tid; i < inside; i += NT) put(i, zero);
+                    if (tid < edges) from_float(out + slice.edge(tid), 0.0f);
+                }
+            }
+            if (lister && r + step < a.rows) fetch_list(a, r + step, slots, list_id, list_v);
+            if (LOSS && lister) for (int e = lane; e < slots; e += 32) unflag(e);
+            __syncthreads();
+            continue;
+        }
+        Scale k;
+        float rest;
+        if constexpr (LOSS) {
+            float s_rest, s_all, m = lowest(), s = 0.0f;
+            double dot = 0.0;
+            float entropy = 0.0f, mass = 0.0f, norm = 1.0f;
+            // everybody's (m, s) against the list's: the largest m as R, the sums relative to it
+            auto totals = [&]() {
+                const float wm = group_max<32>(m);
+                const float ws = group_sum<32>(s * exp2_fast(m - wm));
+                if (lister) dot = warp_sum_double(dot);
+                if (lane == 0) {
+                    if (lister) { list_part[turn] = make_float2(wm, ws); dot_part[turn] = dot; }
+                    else part[turn][warp] = make_float2(wm, ws);
+                }
+                __syncwarp();
+                if (C > 1) cluster_sync(); else __syncthreads();
+                float2 of_list = make_float2(lowest(), 0.0f);
+                float top = lowest();
+                for (int i = lane; i < C * NW; i += 32) top = fmaxf(top, (C > 1 ? cluster_load2(&part[turn][i % NW], i / NW) : part[turn][i]).x);
+                if (lane < C) of_list = C > 1 ? cluster_load2(&list_part[turn], lane) : list_part[turn];
+                k.R = group_max<32>(fmaxf(top, of_list.x));
+                float sum = 0.0f;
+                for (int i = lane; i < C * NW; i += 32) {
+                    const float2 v = C > 1 ? cluster_load2(&part[turn][i % NW], i / NW) : part[turn][i];
+                    sum += v.y * exp2_fast(v.x - k.R);
+                }
+                s_rest = group_sum<32>(sum);
+                s_all = s_rest + group_sum<32>(of_list.y * exp2_fast(of_list.x - k.R));
+                if (lister && rank == 0) {
+                    dot = lane < C ? (C > 1 ? cluster_load_double(&dot_part[turn], lane) : dot_part[turn]) : 0.0;
+                    dot = warp_sum_double(dot);
+                }
+                turn ^= 1;
+            };
+            // listed elements of a vector become -Inf
+            auto mask = [&](uint4& q, uint32_t f) {
+                uint32_t v[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+                for (int j = 0; j < V; ++j)
+                    if (f >> j & 1u) {
+                        if constexpr (DT == kF32) v[j] = 0xFF800000u;
+                        else v[j / 2] = j & 1 ? (v[j / 2] & 0xFFFFu) | 0xFF800000u : (v[j / 2] & 0xFFFF0000u) | 0xFF80u;
+                    }
+                q = make_uint4(v[0], v[1], v[2], v[3]);
+            };
+            // this thread's vectors, listed elements masked, a block at a time (absent vectors are -Inf)
+            auto each = [&](auto&& use, bool keep) {
+                walk(0, [&](uint4 (&now)[U], int b) {
+                    const int i0 = b * (NT * U) + tid;
+                    const uint8_t* fl = flags + i0;
+                    uint32_t f[U];
+                    if (b < whole) {
+#pragma unroll
+                        for (int u = 0; u < U; ++u) f[u] = fl[u * NT];
+                    } else {
+#pragma unroll
+                        for (int u = 0; u < U; ++u) f[u] = i0 + u * NT < inside ? fl[u * NT] : 0u;
+                    }
+                    if (keep && b < plan.stash) {
+#pragma unroll
+                        for (int u = 0; u < U; ++u) stash[i0 + u * NT] = now[u];
+                    }
+                    if ((f[0] | f[1] | f[2] | f[3]) != 0u) {
+#pragma unroll
+                        for (int u = 0; u < U; ++u) if (f[u] != 0u) mask(now[u], f[u]);
+                    }
+                    use(now);
+                });
+                if (tid < edges) {                        // at most one element a thread, as a vector of its own
+                    const long long c = slice.edge(tid);
+                    bool listed = false;
+                    for (int e = 0; e < slots; ++e) listed |= list_at[e] == c;
+                    uint4 now[U];
+#pragma unroll
+                    for (int u = 0; u < U; ++u) now[u] = make_uint4(RowType<DT>::kLow, RowType<DT>::kLow, RowType<DT>::kLow, RowType<DT>::kLow);
+                    if (!listed) {
+                        if constexpr (DT == kF32) now[0].x = __float_as_uint(row.base[c]);
+                        else now[0].x = (RowType<DT>::kLow & 0xFFFF0000u) | (uint32_t)__bfloat16_as_ushort(row.base[c]);
+                    }
+                    use(now);
+                }
+            };
+            if (lister) {
+                List list;
+                list.load(list_id, list_v, slots);
+                list.probabilities(a, weight, a.teacher_lse ? a.teacher_lse[r] : 0.0f, inv_t, (float)(1.0 / (double)a.temperature - (double)inv_t));
+                entropy = list.entropy; mass = list.mass; norm = list.norm;
+                float z[kEntries];
+#pragma unroll
+                for (int e = 0; e < kEntries; ++e) {
+                    if (e * 32 >= slots) break;
+                    const int id = list_at[e * 32 + lane];
+                    z[e] = id >= 0 ? to_float(row.base[id]) : -INFINITY;
+                    list_p[e * 32 + lane] = list.p[e];
+                    list_z[e * 32 + lane] = z[e];
+                    m = fmaxf(m, z[e] * c2);
+                    if (id >= 0 && list.p[e] != 0.0f) dot += (double)list.p[e] * z[e];
+                }
+#pragma unroll
+                for (int e = 0; e < kEntries; ++e) {
+                    if (e * 32 >= slots) break;
+                    s += exp2_fast(fmaf(z[e], c2, -m));
+                }
+                if (lane == 0) rest_s = list.rest;
+            } else {
+                float2 add = make_float2(0.0f, 0.0f);
+                const float2 cc = make_float2(c2, c2);
+                each([&](const uint4 (&now)[U]) {
+                    float top = vector_max<DT>(now[0]);
+#pragma unroll
+                    for (int u = 1; u < U; ++u) top = fmaxf(top, vector_max<DT>(now[u]));
+                    const float old = m;
+                    m = fmaxf(m, top * c2);
+                    const float move = exp2_fast(old - m);
+                    add = __fmul2_rn(add, make_float2(move, move));
+                    const float2 mm = make_float2(-m, -m);
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        float v[V];
+                        unpack_vector<DT>(now[u], v);
+#pragma unroll
+                        for (int j = 0; j < V; j += 2) {
+                            const float2 x = __ffma2_rn(make_float2(v[j], v[j + 1]), cc, mm);
+                            add = __fadd2_rn(add, make_float2(exp2_fast(x.x), exp2_fast(x.y)));
+                        }
+                    }
+                }, GRAD);
+                s = add.x + add.y;
+            }
+            totals();
+            k.slow = !(fabsf(k.R) < 1e30f);
+            if (k.slow) {
+                // logits so large or small that their scaled form leaves the range: the largest one as it is, then the sums
+                const double all_dot = dot;
+                m = lowest(); s = 0.0f; dot = 0.0;
+                if (lister) { for (int e = lane; e < slots; e += 32) m = fmaxf(m, list_z[e]); }
+                else { if (blocks > 0) fetch(even, vec, 0); each([&](const uint4 (&now)[U]) { for (int u = 0; u < U; ++u) m = fmaxf(m, vector_max<DT>(now[u])); }, false); }
+                totals();
+                const float M = k.R;
+                m = 0.0f; s = 0.0f; dot = 0.0;
+                if (lister) { for (int e = lane; e < slots; e += 32) s += exp2_fast((list_z[e] - M) * c2); }
+                else {
+                    if (blocks > 0) fetch(even, vec, 0);
+                    each([&](const uint4 (&now)[U]) {
+                        for (int u = 0; u < U; ++u) {
+                            float v[V];
+                            unpack_vector<DT>(now[u], v);
+                            for (int j = 0; j < V; ++j) s += exp2_fast((v[j] - M) * c2);
+                        }
+                    }, false);
+                }
+                totals();
+                k.R = M;
+                dot = all_dot;
+            }
+            rest = rest_s;
+            k.inv = 1.0f / s_all;
+            k.off = rest > 0.0f && s_rest > 0.0f ? 1.0f - rest * s_all / s_rest : 1.0f;
+            if (lister) {
+                for (int e = lane; e < slots; e += 32) unflag(e);
+                __syncwarp();
+                if (r + step < a.rows) fetch_list(a, r + step, slots, list_id, list_v);
+            }
+            if (lister && rank == 0) {
+                float lse, log_rest;
+                const double inv_t_d = 1.0 / (double)a.temperature;
+                const float loss = row_loss(entropy, mass, norm, rest, dot, inv_t_d, k.slow ? k.R * inv_t_d : k.R * plan.kappa * kLn2D, s_all, s_rest, lse, log_rest);
+                if (lane == 0) {
+                    a.loss[r] = loss * weight * a.scale;
+                    if (!GRAD && a.stats) { a.stats[2 * r] = lse; a.stats[2 * r + 1] = a.teacher_lse ? log_rest : 0.0f; }
+                }
+            }
+        } else {
+            rest = rest_s;
+            k = scale_of_stats(a.stats[2 * r], a.stats[2 * r + 1], rest);
+            if (lister && r + step < a.rows) fetch_list(a, r + step, slots, list_id, list_v);
+        }
+        if constexpr (GRAD) {
+            const float up = weight * a.scale * (!LOSS && a.grad_loss ? a.grad_loss[r] : 1.0f) * inv_t, scale = up * k.off * k.inv;
+            if (!lister) {
+                const int kept = LOSS ? plan.stash : 0;
+                if (LOSS && blocks > 0) fetch(even, kept > 0 ? stash : vec, 0);
+                const float2 cc = make_float2(c2, c2), rr = make_float2(-k.R, -k.R), ss = make_float2(scale, scale);
+                auto pass = [&](auto&& power2) {
+                    walk(kept, [&](uint4 (&now)[U], int b) {
+                        const int i0 = b * (NT * U) + tid;
+#pragma unroll
+                        for (int u = 0; u < U; ++u) {
+                            float v[V];
+                            uint32_t q[4];
+                            unpack_vector<DT>(now[u], v);
+#pragma unroll
+                            for (int j = 0; j < V; j += 2) {
+                                const float2 g = __fmul2_rn(power2(make_float2(v[j], v[j + 1])), ss);
+                                v[j] = g.x; v[j + 1] = g.y;
+                            }
+                            pack_words<DT, 4>(v, q);
+                            if (b < whole || i0 + u * NT < inside) put(i0 + u * NT, q);
+                        }
+                    });
+                };
+                if (!k.slow) pass([&](float2 z) { const float2 x = __ffma2_rn(z, cc, rr); return make_float2(exp2_fast(x.x), exp2_fast(x.y)); });
+                else pass([&](float2 z) { return make_float2(power_of<LOSS>(z.x, k.R, true, c2, inv_t), power_of<LOSS>(z.y, k.R, true, c2, inv_t)); });
+                if (tid < edges) from_float(out + slice.edge(tid), scale * power_of<LOSS>(to_float(row.base[slice.edge(tid)]), k.R, k.slow, c2, inv_t));
+            }
+            __syncthreads();
+            if (lister)
+                for (int e = lane; e < slots; e += 32)
+                    if (list_at[e] >= 0) from_float(out + list_at[e], up * fmaf(power_of<LOSS>(list_z[e], k.R, k.slow, c2, inv_t), k.inv, -list_p[e]));
+        }
     }
+    if (LOSS && C > 1) cluster_sync();                    // nobody's shared memory goes while others may still read it
+}
+
+template <int DT, bool LOSS, bool GRAD, int NT> cudaError_t launch_rows(const DistillArgs& a, const RowPlan& plan, cudaStream_t stream) {
+    auto kernel = distill_kernel<DT, LOSS, GRAD, NT>;
+    static PerDeviceOnce once;
+    cudaError_t e = once.run([&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRowSmem); });
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.blockDim = dim3(NT + 32);
+    cfg.gridDim = dim3((unsigned)plan.cluster);
+    cfg.dynamicSmemBytes = (size_t)plan.flags + (size_t)plan.stash * NT * kBlockVectors * 16;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)plan.cluster; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    // clusters that the device holds at once: asked again only when this thread's last answer was for another shape
+    static thread_local struct { int dev, cluster, clusters; size_t smem; } last = {-1, 0, 0, 0};
+    int dev = 0;
+    if ((e = cudaGetDevice(&dev)) != cudaSuccess) return e;
+    if (last.dev != dev || last.cluster != plan.cluster || last.smem != cfg.dynamicSmemBytes) {
+        int clusters = 0;
+        if ((e = cudaOccupancyMaxActiveClusters(&clusters, kernel, &cfg)) != cudaSuccess) return e;
+        last = {dev, plan.cluster, clusters < 1 ? 1 : clusters, cfg.dynamicSmemBytes};
+    }
+    cfg.gridDim = dim3((unsigned)(std::min<long long>(a.rows, last.clusters) * plan.cluster));
+    return cudaLaunchKernelEx(&cfg, kernel, a, plan);
+}
+
+template <int DT, bool LOSS, bool GRAD, int NT> cudaError_t launch_as(const DistillArgs& a, RowPlan plan, cudaStream_t stream) {
+    // A third of an SM's shared memory for the stash, the least that three blocks leave each other
+    constexpr int kBlockBytes = NT * kBlockVectors * 16, kStashBytes = 64 * 1024;
+    plan.stash = LOSS && GRAD ? std::max(0, std::min(plan.slice_vectors / (NT * kBlockVectors), (kStashBytes - plan.flags) / kBlockBytes)) : 0;
+    return launch_rows<DT, LOSS, GRAD, NT>(a, plan, stream);
 }
 
 template <bool LOSS, bool GRAD> cudaError_t launch(const DistillArgs& a, int dtype, int sms, cudaStream_t stream) {
-    const unsigned grid = (unsigned)std::min<long long>(a.rows, 4ll * sms);
-    if (dtype == kF32) wide_distill_kernel<kF32, LOSS, GRAD><<<grid, kWideThreads, 0, stream>>>(a);
-    else wide_distill_kernel<kBF16, LOSS, GRAD><<<grid, kWideThreads, 0, stream>>>(a);
-    return cudaGetLastError();
+    const int e = dtype == kF32 ? 4 : 2, V = 16 / e;
+    const long long vectors = std::max<long long>(1, (a.vocab + 2 * V - 2) / V);      // of a row, wherever it starts
+    RowPlan plan;
+    plan.slots = (a.k + 31) / 32 * 32;
+    plan.kappa = kLog2eD / a.temperature / (double)(float)(kLog2eD / a.temperature);
+    // Several blocks to a row where the rows alone do not fill the device (a row of 131072 bf16 logits: 14 us on one block, 11.4 us on
+    // eight), and where a row is longer than 256 KB
+    plan.cluster = 1;
+    while (plan.cluster < kMaxCluster && (vectors + plan.cluster - 1) / plan.cluster > 16500) plan.cluster *= 2;
+    while (plan.cluster < kMaxCluster && a.rows * plan.cluster * 2 <= sms && vectors / plan.cluster > 256) plan.cluster *= 2;
+    plan.slice_vectors = (int)((vectors + plan.cluster - 1) / plan.cluster);
+    plan.flags = LOSS ? (plan.slice_vectors + 15) / 16 * 16 : 0;
+    // Short rows by small blocks, of which more are under way (4096 x 4000 fp32, loss and gradient: 63 us with 128 threads, 91 with 256);
+    // long ones by larger blocks, with more loads in flight than rows (300 x 32001 fp32: 28 and 24 us)
+    const bool small = vectors <= 2048 && a.rows > 2ll * sms;
+    if (dtype == kF32) return small ? launch_as<kF32, LOSS, GRAD, 128>(a, plan, stream) : launch_as<kF32, LOSS, GRAD, 256>(a, plan, stream);
+    return small ? launch_as<kBF16, LOSS, GRAD, 128>(a, plan, stream) : launch_as<kBF16, LOSS, GRAD, 256>(a, plan, stream);
 }
 
 }  // namespace

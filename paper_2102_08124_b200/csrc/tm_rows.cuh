@@ -11,9 +11,10 @@
 namespace tmask {
 
 // DT = kF32 or kBF16: storage type, element size, elements of a 16-byte vector
+// (and a word of -Inf)
 template <int DT> struct RowType;
-template <> struct RowType<kF32> { using T = float; static constexpr int kBytes = 4, kVec = 4; };
-template <> struct RowType<kBF16> { using T = __nv_bfloat16; static constexpr int kBytes = 2, kVec = 8; };
+template <> struct RowType<kF32> { using T = float; static constexpr int kBytes = 4, kVec = 4; static constexpr uint32_t kLow = 0xFF800000u; };
+template <> struct RowType<kBF16> { using T = __nv_bfloat16; static constexpr int kBytes = 2, kVec = 8; static constexpr uint32_t kLow = 0xFF80FF80u; };
 
 __device__ __forceinline__ float to_float(float v) { return v; }
 __device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
@@ -42,6 +43,34 @@ template <int DT, int WORDS> __device__ __forceinline__ void pack_words(const fl
     }
 }
 
+template <int DT> __device__ __forceinline__ void unpack_vector(const uint4& u, float* v) {
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+    unpack_words<DT, 4>(w, v);
+}
+
+// the largest of a vector's elements; NaN only where all are
+template <int DT> __device__ __forceinline__ float vector_max(const uint4& u) {
+    if constexpr (DT == kF32) return fmaxf(fmaxf(__uint_as_float(u.x), __uint_as_float(u.y)), fmaxf(__uint_as_float(u.z), __uint_as_float(u.w)));
+    else {
+        const __nv_bfloat162 m = __hmax2(__hmax2(reinterpret_cast<const __nv_bfloat162&>(u.x), reinterpret_cast<const __nv_bfloat162&>(u.y)),
+                                         __hmax2(reinterpret_cast<const __nv_bfloat162&>(u.z), reinterpret_cast<const __nv_bfloat162&>(u.w)));
+        const uint32_t w = reinterpret_cast<const uint32_t&>(m);
+        return fmaxf(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
+    }
+}
+
+// the same, NaN if any is
+__device__ __forceinline__ float max_nan(float a, float b) { float m; asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(a), "f"(b)); return m; }
+template <int DT> __device__ __forceinline__ float vector_max_nan(const uint4& u) {
+    if constexpr (DT == kF32) return max_nan(max_nan(__uint_as_float(u.x), __uint_as_float(u.y)), max_nan(__uint_as_float(u.z), __uint_as_float(u.w)));
+    else {
+        const __nv_bfloat162 m = __hmax2_nan(__hmax2_nan(reinterpret_cast<const __nv_bfloat162&>(u.x), reinterpret_cast<const __nv_bfloat162&>(u.y)),
+                                             __hmax2_nan(reinterpret_cast<const __nv_bfloat162&>(u.z), reinterpret_cast<const __nv_bfloat162&>(u.w)));
+        const uint32_t w = reinterpret_cast<const uint32_t&>(m);
+        return max_nan(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
+    }
+}
+
 // A row seen as 16-byte vectors that start on 16-byte boundaries: vector 0 begins `lead` elements before the row.  Only the
 // first and the last vector can reach past the row; they are accessed one element at a time, so that nothing outside the
 // row is touched whatever its alignment.
@@ -58,16 +87,16 @@ template <int DT> struct RowVectors {
     }
     __device__ __forceinline__ long long column(long long i) const { return i * V - lead; }      // of the vector's first element; may be negative
     __device__ __forceinline__ bool full(long long i) const { return column(i) >= 0 && column(i) + V <= n; }
-    __device__ __forceinline__ void load(long long i, float* v, float fill) const {
+    // the vector as stored; elements outside the row are -Inf
+    __device__ __forceinline__ uint4 load(long long i) const {
         const long long c = column(i);
-        if (full(i)) {
-            const uint4 u = *reinterpret_cast<const uint4*>(base + c);
-            const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-            unpack_words<DT, 4>(w, v);
-        } else {
+        if (full(i)) return *reinterpret_cast<const uint4*>(base + c);
+        float v[V];
 #pragma unroll
-            for (int j = 0; j < V; ++j) v[j] = (c + j >= 0 && c + j < n) ? to_float(base[c + j]) : fill;
-        }
+        for (int j = 0; j < V; ++j) v[j] = (c + j >= 0 && c + j < n) ? to_float(base[c + j]) : -INFINITY;
+        uint32_t w[4];
+        pack_words<DT, 4>(v, w);
+        return make_uint4(w[0], w[1], w[2], w[3]);
     }
     // stores the vector to another row of the same length; `aligned`: that row starts at the same distance from a boundary
     __device__ __forceinline__ void store(void* row, bool aligned, long long i, const float* v) const {
@@ -76,13 +105,34 @@ template <int DT> struct RowVectors {
         if (aligned && full(i)) {
             uint32_t w[4];
             pack_words<DT, 4>(v, w);
-            *reinterpret_cast<uint4*>(out + c) = make_uint4(w[0], w[1], w[2], w[3]);
+            __stcs(reinterpret_cast<uint4*>(out + c), make_uint4(w[0], w[1], w[2], w[3]));
         } else {
 #pragma unroll
             for (int j = 0; j < V; ++j)
                 if (c + j >= 0 && c + j < n) from_float(out + c + j, v[j]);
         }
     }
+};
+
+// The part [from, to) of a row's vectors (to <= its count) that one thread block works on: `inside` full vectors from `vec` on, at
+// element `column`, and up to V - 1 elements in front of them and behind (the row's partial first and last vector, where they
+// belong to this part).  Everything counts in 32 bits.
+template <int DT> struct RowPart {
+    using T = typename RowType<DT>::T;
+    static constexpr int V = RowType<DT>::kVec;
+    long long column;          // of the first full vector
+    int inside, head, tail;    // vectors; elements before and after them
+    __device__ __forceinline__ RowPart(const RowVectors<DT>& row, long long from, long long to) {
+        const long long a = max(0ll, row.column(from)), b = min(row.n, row.column(to));
+        const long long first = row.lead ? max(from, 1ll) : from, last = row.column(to) > row.n ? to - 1 : to;
+        if (a >= b) { column = 0; inside = head = tail = 0; return; }
+        inside = (int)max(0ll, last - first);
+        column = inside > 0 ? row.column(first) : b;
+        head = (int)(column - a);
+        tail = inside > 0 ? (int)(b - (column + (long long)inside * V)) : 0;
+    }
+    // element k of the head and tail together, k < head + tail: its column
+    __device__ __forceinline__ long long edge(int k) const { return k < head ? column - head + k : column + (long long)inside * V + (k - head); }
 };
 
 // 2^x, flushed to zero below the normal range: one instruction, relative error below 2^-22
@@ -98,9 +148,15 @@ template <int WIDTH> __device__ __forceinline__ float group_sum(float v) {
     return v;
 }
 template <int WIDTH> __device__ __forceinline__ float group_max(float v) {
+    if constexpr (WIDTH == 32) {                          // one instruction for a whole warp
+        float m;
+        asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(m) : "f"(v));
+        return m;
+    } else {
 #pragma unroll
-    for (int o = WIDTH / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, o, WIDTH));
-    return v;
+        for (int o = WIDTH / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, o, WIDTH));
+        return v;
+    }
 }
 
 // Sum over the TPR threads of a row (a power of two; the CTA holds one row where TPR > 32).  `buf` holds TPR / 32 floats, and
@@ -114,6 +170,32 @@ template <int TPR> __device__ __forceinline__ float row_sum(float v, float* buf)
         const float t = (threadIdx.x & 31) < TPR / 32 ? buf[threadIdx.x & 31] : 0.0f;
         return group_sum<32>(t);
     }
+}
+
+// Thread-block clusters: this block's rank, a barrier among all their threads, and reads of another block's shared memory
+__device__ __forceinline__ uint32_t cluster_rank() { uint32_t r; asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return r; }
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t cluster_map(const void* shared, uint32_t rank) {
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"((uint32_t)__cvta_generic_to_shared(shared)), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ float2 cluster_load2(const float2* shared, uint32_t rank) {
+    float2 v;
+    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(cluster_map(shared, rank)) : "memory");
+    return v;
+}
+__device__ __forceinline__ unsigned long long cluster_load64(const unsigned long long* shared, uint32_t rank) {
+    unsigned long long v;
+    asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(cluster_map(shared, rank)) : "memory");
+    return v;
+}
+__device__ __forceinline__ double cluster_load_double(const double* shared, uint32_t rank) {
+    double v;
+    asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(v) : "r"(cluster_map(shared, rank)) : "memory");
+    return v;
 }
 
 }  // namespace tmask

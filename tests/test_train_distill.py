@@ -148,6 +148,22 @@ def test_distill(vocab, dtype, tail):
 
 
 @pytest.mark.parametrize("tail", [False, True])
+@pytest.mark.parametrize("rows,vocab,k,dtype", [(5000, 301, 9, "f32"), (4100, 1000, 40, "bf16"), (1501, 4099, 20, "bf16"), (900, 16384, 64, "f32"), (620, 40001, 33, "bf16")])
+def test_more_rows_than_the_device_holds(rows, vocab, k, dtype, tail):
+    """Every thread block has many rows, idle ones among them."""
+    rng = np.random.Generator(np.random.PCG64(rows))
+    values, ids = _lists(rng, rows, vocab, k)
+    ids[rng.random(rows) < 0.1, k // 2:] = -1
+    ids[rng.random(rows) < 0.05] = -1
+    weight = np.where(rng.random(rows) < 0.2, 0.0, rng.uniform(0.5, 1.5, rows)).astype(np.float32)
+    z, zd = _matrix(rng.standard_normal((rows, vocab), dtype=np.float32) * 2, dtype)
+    lse = np.array([ref.log_sum_exp(v.astype(np.float64) / 1.5) + 0.2 for v in values], np.float32) if tail else None
+    _check_distill(z, zd, values, ids, lse, weight, 1.5, 1.0, dtype, inplace=tail)
+    if tail:
+        _check_top(z, zd, k, 1.5)
+
+
+@pytest.mark.parametrize("tail", [False, True])
 @pytest.mark.parametrize("vocab", [40, 3001, 40000])
 def test_bad_and_repeated_ids(vocab, tail):
     rng = np.random.Generator(np.random.PCG64(21))
