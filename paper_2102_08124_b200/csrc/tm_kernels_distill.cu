@@ -233,7 +233,7 @@ __global__ void __launch_bounds__(NT + 32, kBlocks<NT>) distill_kernel(const Dis
     for (int i = tid; i < plan.flags / 16; i += NT + 32) reinterpret_cast<uint4*>(flags)[i] = make_uint4(0u, 0u, 0u, 0u);
     int turn = 0;
     float next_weight = 1.0f;                                             // read a row ahead, as is the list
-    uint4 even[U], odd[U];
+    uint4 w[U];
     const long long start = blockIdx.x / C;
     if (start < a.rows) {
         if (a.row_weight) next_weight = a.row_weight[start];
@@ -250,8 +250,7 @@ __global__ void __launch_bounds__(NT + 32, kBlocks<NT>) distill_kernel(const Dis
         T* const out = GRAD ? static_cast<T*>(a.dlogits) + r * a.ld_d : nullptr;
         const float weight = next_weight;
         if (a.row_weight && r + step < a.rows) next_weight = a.row_weight[r + step];
-        // A thread's vectors come in blocks of U, NT apart; all blocks but the last are whole.  Two register blocks take turns, so that
-        // one is on its way while the other is worked on; the first is on its way while the list is read.
+        // A thread's vectors come in blocks of U, NT apart; all blocks but the last are whole.  The first one is on its way while the list is read.
         const int whole = inside / (NT * U), blocks = (inside + NT * U - 1) / (NT * U);
         auto fetch = [&](uint4 (&w)[U], const uint4* src, int b) {
             src += b * (NT * U) + tid;
@@ -266,15 +265,12 @@ __global__ void __launch_bounds__(NT + 32, kBlocks<NT>) distill_kernel(const Dis
                 }
             }
         };
-        // use(block, its number) for all of this thread's blocks, the first `kept` of them from the stash; block 0 is in `even`
+        // use(block, its number) for all of this thread's blocks, the first `kept` of them from the stash; block 0 is in `w`
         auto walk = [&](int kept, auto&& use) {
-            for (int b = 0; b < blocks;) {
-                if (b + 1 < blocks) fetch(odd, b + 1 < kept ? stash : vec, b + 1);
-                use(even, b);
-                if (++b == blocks) break;
-                if (b + 1 < blocks) fetch(even, b + 1 < kept ? stash : vec, b + 1);
-                use(odd, b);
-                ++b;
+#pragma unroll 1
+            for (int b = 0; b < blocks; ++b) {
+                if (b > 0) fetch(w, b < kept ? stash : vec, b);
+                use(w, b);
             }
         };
         if (lister) {
@@ -308,7 +304,7 @@ __global__ void __launch_bounds__(NT + 32, kBlocks<NT>) distill_kernel(const Dis
                     }
             }
         } else {
-            if (weight != 0.0f && blocks > 0) fetch(even, vec, 0);
+            if (weight != 0.0f && blocks > 0) fetch(w, vec, 0);
         }
         __syncthreads();
         const bool on = on_s;
@@ -481,13 +477,13 @@ __global__ void __launch_bounds__(NT + 32, kBlocks<NT>) distill_kernel(const Dis
                 const double all_dot = dot;
                 m = lowest(); s = 0.0f; dot = 0.0;
                 if (lister) { for (int e = lane; e < slots; e += 32) m = fmaxf(m, list_z[e]); }
-                else { if (blocks > 0) fetch(even, vec, 0); each([&](const uint4 (&now)[U]) { for (int u = 0; u < U; ++u) m = fmaxf(m, vector_max<DT>(now[u])); }, false); }
+                else { if (blocks > 0) fetch(w, vec, 0); each([&](const uint4 (&now)[U]) { for (int u = 0; u < U; ++u) m = fmaxf(m, vector_max<DT>(now[u])); }, false); }
                 totals();
                 const float M = k.R;
                 m = 0.0f; s = 0.0f; dot = 0.0;
                 if (lister) { for (int e = lane; e < slots; e += 32) s += exp2_fast((list_z[e] - M) * c2); }
                 else {
-                    if (blocks > 0) fetch(even, vec, 0);
+                    if (blocks > 0) fetch(w, vec, 0);
                     each([&](const uint4 (&now)[U]) {
                         for (int u = 0; u < U; ++u) {
                             float v[V];
@@ -526,7 +522,7 @@ __global__ void __launch_bounds__(NT + 32, kBlocks<NT>) distill_kernel(const Dis
             const float up = weight * a.scale * (!LOSS && a.grad_loss ? a.grad_loss[r] : 1.0f) * inv_t, scale = up * k.off * k.inv;
             if (!lister) {
                 const int kept = LOSS ? plan.stash : 0;
-                if (LOSS && blocks > 0) fetch(even, kept > 0 ? stash : vec, 0);
+                if (LOSS && blocks > 0) fetch(w, kept > 0 ? stash : vec, 0);
                 const float2 cc = make_float2(c2, c2), rr = make_float2(-k.R, -k.R), ss = make_float2(scale, scale);
                 auto pass = [&](auto&& power2) {
                     walk(kept, [&](uint4 (&now)[U], int b) {

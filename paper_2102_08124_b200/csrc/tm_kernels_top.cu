@@ -3,14 +3,15 @@
 // Order: a logit is the 64-bit whole number (its value's pattern made monotone, then the index from above), so that equal values go
 // by the lower index and no two entries are equal.  -0 counts as +0; NaN is above everything.
 //
-// Bound: HBM (a logit is read once; about four instructions each, one of them an exponential).  A thread block goes through its row --
-// or its slice of one, where a cluster shares a row -- with a running maximum and sum for the softmax and a bound below which no
-// logit can be among the k largest: at first the k-th largest of the threads' maxima over the first block of vectors, later the
-// k-th largest entry so far.  A vector whose maximum is below the bound costs one comparison.  Entries that pass go to a buffer in
-// shared memory; when it holds more than a few hundred, a radix selection over it leaves k and raises the bound (a row of random
-// logits does that once or twice).  A row that overruns the buffer between two looks at it, rising values for instance, goes again
-// with a look after every vector, between which the buffer cannot overrun.
+// Bound: HBM (about six instructions a logit, one of them an exponential).  A thread block goes through its row -- or its slice of
+// one, where a cluster shares a row -- twice.  Pass 1 takes the softmax's running maximum and sum and every thread's largest logit.
+// The k-th largest of those is a bound that at least k logits reach, and few more do (of 131072 random ones and k = 64 some 75).
+// Pass 2 collects the logits that reach it: a comparison for a vector.  What shared memory had room for in pass 1 comes from there,
+// the rest from L2, so that HBM is read once.  The entries are then put in order by counting, for each, the larger ones.
+// Where far more reach the bound than the buffer holds (few threads have seen all the large ones), the vectors are gone through
+// again one of each thread at a time, a radix selection cutting the buffer back to k, and raising the bound, whenever it fills up.
 #include <algorithm>
+#include <cstdlib>
 
 #include "tm_launch.h"
 #include "tm_rows.cuh"
@@ -20,7 +21,8 @@ namespace tmask {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr int kMaxCluster = 8, kBlockVectors = 4, kLook = 640;     // kLook: entries above which the buffer is cut back to k
+constexpr int kMaxCluster = 8, kBlockVectors = 4;
+constexpr int kLook = 640;     // entries above which the buffer is cut back to k
 
 __device__ __forceinline__ uint32_t order_of(float v) {
     if (v != v) return 0xFFFFFFFFu;
@@ -35,65 +37,161 @@ __device__ __forceinline__ unsigned long long entry_of(float v, long long column
 }
 
 struct TopPlan {
-    int cluster;
+    int cluster, stash;            // stash: blocks of NT * U vectors that stay in shared memory between the passes
     long long slice_vectors;
     double kappa;                  // (log2(e) / T) / c2, the rounding of c2
 };
 
 // entries of the buffer: kLook, what one vector of every thread can add and the row's edges, at least; and the lists of a cluster
-template <int DT, int NT> constexpr int kCapacity = std::max(kLook + NT * RowType<DT>::kVec + 32, kTopMax * (kMaxCluster + 1));
+template <int DT, int NT> constexpr int kCapacity = 2 * ((1 + std::max(kLook + NT * RowType<DT>::kVec + 32, kTopMax * (kMaxCluster + 1))) / 2);
 
-// The k-th largest of buf[0, n), n > k > 0, by 8-bit digits from the top; all threads, which get the same answer.
-template <int NT> struct Selection {
+// A block's list under way, in shared memory
+struct Work {
     unsigned int hist[256];
-    unsigned long long prefix;
+    unsigned long long found[kTopMax], prefix;
     unsigned int left, done;
-    __device__ __forceinline__ unsigned long long operator()(const unsigned long long* buf, int n, int k) {
-        const int tid = threadIdx.x, lane = tid & 31;
-        if (tid == 0) { prefix = 0; left = (unsigned)k; done = 0; }
-        for (int digit = 7; digit >= 0; --digit) {
-            for (int b = tid; b < 256; b += NT) hist[b] = 0;
-            __syncthreads();
-            const unsigned long long known = prefix, care = digit == 7 ? 0ull : ~0ull << (8 * (digit + 1));
-            for (int i = tid; i < n; i += NT) {
-                const unsigned long long e = buf[i];
-                if ((e & care) == known) atomicAdd(&hist[(e >> (8 * digit)) & 255], 1u);
-            }
-            __syncthreads();
-            if (tid < 32) {
-                // lane l has bins 255 - 8 l downwards: how many entries lie in the lanes before it
-                unsigned int own = 0;
-                for (int b = 0; b < 8; ++b) own += hist[255 - 8 * lane - b];
-                unsigned int before = own;
-#pragma unroll
-                for (int o = 1; o < 32; o <<= 1) { const unsigned int t = __shfl_up_sync(0xFFFFFFFFu, before, o); if (lane >= o) before += t; }
-                before -= own;
-                const unsigned int want = left;
-                __syncwarp();
-                if (before < want && want <= before + own) {
-                    unsigned int need = want - before;
-                    int b = 255 - 8 * lane;
-                    while (hist[b] < need) need -= hist[b--];
-                    prefix = known | ((unsigned long long)b << (8 * digit));
-                    left = need;
-                    done = hist[b] == need;               // the whole bin is among the largest: lower digits may be anything
-                }
-            }
-            __syncthreads();
-            if (done) break;
-        }
-        return prefix;
-    }
+    int count, kept;               // entries of the buffer
 };
 
-template <int DT, int NT> __global__ void __launch_bounds__(NT, NT == 256 ? 4 : 8) top_kernel(const TopArgs a, const TopPlan plan) {
+// Cuts buf[0, w.count) back to its `have` largest (0 < have < w.count) and returns a number that exactly they reach: a radix
+// selection by 8-bit digits from the top.  All threads; out of line, for its size.
+template <int NT> __device__ __noinline__ unsigned long long cut_back(unsigned long long* buf, Work& w, int have) {
+    const int tid = threadIdx.x, lane = tid & 31, n = w.count;
+    if (tid == 0) { w.prefix = 0; w.left = (unsigned)have; w.done = 0; w.kept = 0; }
+    for (int digit = 7; digit >= 0; --digit) {
+        for (int b = tid; b < 256; b += NT) w.hist[b] = 0;
+        __syncthreads();
+        const unsigned long long known = w.prefix, care = digit == 7 ? 0ull : ~0ull << (8 * (digit + 1));
+        for (int i = tid; i < n; i += NT) {
+            const unsigned long long e = buf[i];
+            if ((e & care) == known) atomicAdd(&w.hist[(e >> (8 * digit)) & 255], 1u);
+        }
+        __syncthreads();
+        if (tid < 32) {
+            // lane l has bins 255 - 8 l downwards: how many entries lie in the lanes before it
+            unsigned int own = 0;
+            for (int b = 0; b < 8; ++b) own += w.hist[255 - 8 * lane - b];
+            unsigned int before = own;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) { const unsigned int t = __shfl_up_sync(0xFFFFFFFFu, before, o); if (lane >= o) before += t; }
+            before -= own;
+            const unsigned int want = w.left;
+            __syncwarp();
+            if (before < want && want <= before + own) {
+                unsigned int need = want - before;
+                int b = 255 - 8 * lane;
+                while (w.hist[b] < need) need -= w.hist[b--];
+                w.prefix = known | ((unsigned long long)b << (8 * digit));
+                w.left = need;
+                w.done = w.hist[b] == need;               // the whole bin is among the largest: lower digits may be anything
+            }
+        }
+        __syncthreads();
+        if (w.done) break;
+    }
+    const unsigned long long kth = w.prefix;
+    for (int i = tid; i < n; i += NT) if (buf[i] >= kth) w.found[atomicAdd(&w.kept, 1)] = buf[i];
+    __syncthreads();
+    for (int i = tid; i < have; i += NT) buf[i] = w.found[i];
+    if (tid == 0) w.count = have;
+    __syncthreads();
+    return kth;
+}
+
+// value below which no entry reaches `bound` (-Inf: none)
+__device__ __forceinline__ float bound_value(unsigned long long bound) {
+    const uint32_t key = (uint32_t)(bound >> 32);
+    return key <= 0x007FFFFFu ? -INFINITY : value_of(key);                            // -Inf itself is 0x007FFFFF
+}
+
+// A number that at least k of the threads' keys reach, and hardly more: the k-th largest by its upper 16 bits.  All threads.
+template <int NT> __device__ __noinline__ uint32_t bound_of_keys(uint32_t key, int k, Work& w) {
+    const int tid = threadIdx.x, lane = tid & 31;
+    if (tid == 0) { w.prefix = 0; w.left = (unsigned)k; }
+    for (int digit = 3; digit >= 2; --digit) {
+        for (int b = tid; b < 256; b += NT) w.hist[b] = 0;
+        __syncthreads();
+        const uint32_t known = (uint32_t)w.prefix;
+        if (digit == 3 || (key >> 24) == known >> 24) atomicAdd(&w.hist[(key >> (8 * digit)) & 255], 1u);
+        __syncthreads();
+        if (tid < 32) {
+            unsigned int own = 0;
+            for (int b = 0; b < 8; ++b) own += w.hist[255 - 8 * lane - b];
+            unsigned int before = own;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) { const unsigned int t = __shfl_up_sync(0xFFFFFFFFu, before, o); if (lane >= o) before += t; }
+            before -= own;
+            const unsigned int want = w.left;
+            __syncwarp();
+            if (before < want && want <= before + own) {
+                unsigned int need = want - before;
+                int b = 255 - 8 * lane;
+                while (w.hist[b] < need) need -= w.hist[b--];
+                w.prefix = known | ((uint32_t)b << (8 * digit));
+                w.left = need;
+            }
+        }
+        __syncthreads();
+    }
+    return (uint32_t)w.prefix;
+}
+
+// The entries of a vector at or above the bound, into the buffer as far as it has room.  Out of line: few vectors get here.
+template <int DT> __device__ __noinline__ void offer_vector(uint4 q, float least, unsigned long long bound, long long column, unsigned long long* buf, int room, int* count) {
+    constexpr int V = RowType<DT>::kVec;
+    float v[V];
+    unpack_vector<DT>(q, v);
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        if (v[j] < least) continue;
+        const unsigned long long e = entry_of(v[j], column + j);
+        if (e >= bound) {
+            const int at = atomicAdd(count, 1);
+            if (at < room) buf[at] = e;
+        }
+    }
+}
+
+// Collects the entries at or above the bound one vector of each thread at a time, with a look at the buffer after each.  All threads.
+template <int DT, int NT> __device__ __noinline__ void collect_slowly(unsigned long long* buf, Work& w, const uint4* vec, int inside, unsigned long long bound, long long column,
+                                                                      int have) {
+    constexpr int V = RowType<DT>::kVec;
+    if (threadIdx.x == 0) w.count = 0;
+    __syncthreads();
+    for (int i0 = 0; i0 < inside; i0 += NT) {
+        const int i = i0 + (int)threadIdx.x;
+        bool full = false;
+        if (i < inside) {
+            const uint4 q = vec[i];
+            const float least = bound_value(bound);
+            if (!(vector_max_nan<DT>(q) < least)) {
+                float v[V];
+                unpack_vector<DT>(q, v);
+                for (int j = 0; j < V; ++j)
+                    if (!(v[j] < least)) {
+                        const unsigned long long e = entry_of(v[j], column + (long long)i * V + j);
+                        if (e >= bound) {
+                            const int at = atomicAdd(&w.count, 1);
+                            buf[at] = e;
+                            full |= at >= kLook;
+                        }
+                    }
+            }
+        }
+        if (__syncthreads_or(full)) bound = max(bound, cut_back<NT>(buf, w, have));
+    }
+}
+
+template <int NT> constexpr int kBlocks = 1024 / NT;       // blocks an SM: the registers they may use
+
+template <int DT, int NT> __global__ void __launch_bounds__(NT, kBlocks<NT>) top_kernel(const TopArgs a, const TopPlan plan) {
     using T = typename RowType<DT>::T;
     constexpr int V = RowType<DT>::kVec, NW = NT / 32, U = kBlockVectors, kRoom = kCapacity<DT, NT>;
-    extern __shared__ __align__(16) unsigned long long buf[];             // kRoom entries
-    __shared__ unsigned long long found[kTopMax];
-    __shared__ Selection<NT> select;
+    extern __shared__ __align__(16) unsigned long long buf[];             // kRoom entries, then the stash
+    uint4* const stash = reinterpret_cast<uint4*>(buf + kRoom);
+    __shared__ Work work;
     __shared__ float2 part[2][NW];
-    __shared__ int count_s, kept_s, have_s[2];
+    __shared__ int have_s[2];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int C = plan.cluster;
     const uint32_t rank = C > 1 ? cluster_rank() : 0u;
@@ -108,8 +206,8 @@ template <int DT, int NT> __global__ void __launch_bounds__(NT, NT == 256 ? 4 : 
         const int inside = slice.inside, edges = slice.head + slice.tail;
         const int have = (int)min((long long)a.k, (long long)inside * V + edges);         // entries that this slice can give
         const int blocks = (inside + NT * U - 1) / (NT * U), whole = inside / (NT * U);
-        auto fetch = [&](uint4 (&w)[U], int b) {
-            const uint4* src = vec + b * (NT * U) + tid;
+        auto fetch = [&](uint4 (&w)[U], const uint4* src, int b) {
+            src += b * (NT * U) + tid;
             if (b < whole) {
 #pragma unroll
                 for (int u = 0; u < U; ++u) w[u] = src[u * NT];
@@ -121,57 +219,28 @@ template <int DT, int NT> __global__ void __launch_bounds__(NT, NT == 256 ? 4 : 
                 }
             }
         };
-        // entries at or above `bound` are collected; `bound_f` is its value (or -Inf, which everything passes)
-        unsigned long long bound = 0;
-        float bound_f = -INFINITY, m = -3.4028234663852886e38f, s = 0.0f;
-        bool full = false, over = false;                  // this thread put an entry past kLook, or past the end
-        auto set_bound = [&](unsigned long long b) {
-            bound = b;
-            const uint32_t key = (uint32_t)(b >> 32);
-            bound_f = key <= 0x007FFFFFu ? -INFINITY : value_of(key);                 // -Inf itself is 0x007FFFFF
-        };
-        auto offer = [&](float v, long long column) {
-            const unsigned long long e = entry_of(v, column);
-            if (e >= bound) {
-                const int at = atomicAdd(&count_s, 1);
-                if (at < kRoom) buf[at] = e;
-                full |= at >= kLook;
-                over |= at >= kRoom;
+        // use(block, its number) for all of this thread's blocks, the first `kept` of them from the stash
+        auto walk = [&](int kept, auto&& use) {
+#pragma unroll 1
+            for (int b = 0; b < blocks; ++b) {
+                uint4 w[U];
+                fetch(w, b < kept ? stash : vec, b);
+                use(w, b);
             }
         };
-        // cuts the buffer back to the k largest, whose last one is the new bound; all threads, at a point that all have reached
-        auto cut = [&]() {
-            const int n = count_s;
-            const unsigned long long kth = select(buf, n, have);
-            if (tid == 0) kept_s = 0;
-            __syncthreads();
-            for (int i = tid; i < n; i += NT) if (buf[i] >= kth) found[atomicAdd(&kept_s, 1)] = buf[i];
-            __syncthreads();
-            for (int i = tid; i < have; i += NT) buf[i] = found[i];
-            if (tid == 0) count_s = have;
-            if (kth > bound) set_bound(kth);
-            full = false;
-            __syncthreads();
-        };
-        auto offer_vector = [&](const uint4& q, float top, int i) {
-            if (!(top < bound_f) && i < inside) {
-                float v[V];
-                unpack_vector<DT>(q, v);
+        float m = -3.4028234663852886e38f, s = 0.0f, largest = -INFINITY;
+        walk(0, [&](const uint4 (&w)[U], int b) {
+            if (b < plan.stash) {
 #pragma unroll
-                for (int j = 0; j < V; ++j)
-                    if (!(v[j] < bound_f)) offer(v[j], slice.column + (long long)i * V + j);
+                for (int u = 0; u < U; ++u) stash[b * (NT * U) + u * NT + tid] = w[u];
             }
-        };
-        if (tid == 0) count_s = 0;
-        __syncthreads();
-        bool broken = false;                              // the buffer has overrun: the sums go on, the list comes from a second walk
-        auto step = [&](const uint4 (&w)[U], int b) {
-            float top[U];
+            float top = vector_max_nan<DT>(w[0]);
 #pragma unroll
-            for (int u = 0; u < U; ++u) top[u] = vector_max_nan<DT>(w[u]);
+            for (int u = 1; u < U; ++u) top = max_nan(top, vector_max_nan<DT>(w[u]));
+            largest = max_nan(largest, top);
             if (a.lse) {
                 const float old = m;
-                m = fmaxf(m, fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * c2);
+                m = fmaxf(m, top * c2);
                 const float2 cc = make_float2(c2, c2), mm = make_float2(-m, -m);
                 float2 add = make_float2(s * exp2_fast(old - m), 0.0f);
 #pragma unroll
@@ -186,49 +255,29 @@ template <int DT, int NT> __global__ void __launch_bounds__(NT, NT == 256 ? 4 : 
                 }
                 s = add.x + add.y;
             }
-            if (b == 0 && min(inside, NT) >= a.k) {
-                // at least k threads have a vector: the k-th largest of their maxima, or somewhat less, bounds the k-th largest logit
-                const uint32_t key = tid < inside ? order_of(max_nan(max_nan(top[0], top[1]), max_nan(top[2], top[3]))) : 0u;
-                uint32_t lo = 0u, hi = 0xFFFFFFFFu;
-                for (int q = 0; q < 32 && lo < hi; ++q) {
-                    const uint32_t mid = lo + (hi - lo) / 2 + 1;
-                    const int n = __syncthreads_count(key >= mid);
-                    if (n >= a.k) { lo = mid; if (n <= a.k + a.k / 4) break; } else hi = mid - 1;
-                }
-                set_bound((unsigned long long)lo << 32);
-            }
-            if (broken) return;
-#pragma unroll
-            for (int u = 0; u < U; ++u) offer_vector(w[u], top[u], b * (NT * U) + u * NT + tid);
-            if (__syncthreads_or(full)) {
-                broken = __syncthreads_or(over);
-                if (!broken) cut();
+        });
+        // entries at or above the bound are collected
+        unsigned long long bound = 0;
+        if (tid == 0) work.count = 0;
+        if (min(inside, NT) >= a.k) bound = (unsigned long long)bound_of_keys<NT>(tid < inside ? order_of(largest) : 0u, a.k, work) << 32;
+        else __syncthreads();
+        const float least = bound_value(bound);
+        auto offer = [&](float v, long long column) {
+            const unsigned long long e = entry_of(v, column);
+            if (e >= bound) {
+                const int at = atomicAdd(&work.count, 1);
+                if (at < kRoom) buf[at] = e;
             }
         };
-        {
-            uint4 even[U], odd[U];
-            if (blocks > 0) fetch(even, 0);
-            for (int b = 0; b < blocks;) {
-                if (b + 1 < blocks) fetch(odd, b + 1);
-                step(even, b);
-                if (++b == blocks) break;
-                if (b + 1 < blocks) fetch(even, b + 1);
-                step(odd, b);
-                ++b;
+        walk(plan.stash, [&](const uint4 (&w)[U], int b) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int i = b * (NT * U) + u * NT + tid;
+                if (!(vector_max_nan<DT>(w[u]) < least) && i < inside) offer_vector<DT>(w[u], least, bound, slice.column + (long long)i * V, buf, kRoom, &work.count);
             }
-        }
-        if (broken) {
-            if (tid == 0) count_s = 0;
-            full = over = false;
-            set_bound(0);
-            __syncthreads();
-            for (int i0 = 0; i0 < inside; i0 += NT) {
-                const int i = i0 + tid;
-                const uint4 q = i < inside ? vec[i] : make_uint4(0u, 0u, 0u, 0u);
-                offer_vector(q, vector_max_nan<DT>(q), i);
-                if (__syncthreads_or(full)) cut();
-            }
-        }
+        });
+        __syncthreads();
+        if (work.count > kRoom - 32) collect_slowly<DT, NT>(buf, work, vec, inside, bound, slice.column, have);
         if (tid < edges) {
             const long long c = slice.edge(tid);
             const float v = to_float(row.base[c]), old = m;
@@ -237,15 +286,16 @@ template <int DT, int NT> __global__ void __launch_bounds__(NT, NT == 256 ? 4 : 
             offer(v, c);
         }
         __syncthreads();
-        if (count_s > have) cut();
+        if (work.count > max(have, kTopMax)) cut_back<NT>(buf, work, have);
         // this slice's list, sorted by counting the larger ones, and the warps' sums
-        for (int i = tid; i < have; i += NT) found[i] = buf[i];
+        const int n = work.count;
+        for (int i = tid; i < n; i += NT) work.found[i] = buf[i];
         __syncthreads();
-        for (int i = tid; i < have; i += NT) {
-            const unsigned long long e = found[i];
+        for (int i = tid; i < n; i += NT) {
+            const unsigned long long e = work.found[i];
             int at = 0;
-            for (int j = 0; j < have; ++j) at += found[j] > e;
-            buf[at] = e;
+            for (int j = 0; j < n; ++j) at += work.found[j] > e;
+            if (at < have) buf[at] = e;
         }
         auto post = [&]() {
             const float wm = group_max<32>(m), ws = group_sum<32>(s * exp2_fast(m - wm));
@@ -335,27 +385,33 @@ template <int DT, int NT> __global__ void __launch_bounds__(NT, NT == 256 ? 4 : 
     }
 }
 
-template <int DT, int NT> cudaError_t launch_rows(const TopArgs& a, const TopPlan& plan, cudaStream_t stream) {
+template <int DT, int NT> cudaError_t launch_rows(const TopArgs& a, TopPlan plan, cudaStream_t stream) {
+    // of an SM's 228 KB each block's share, less its buffer and static arrays
+    constexpr int kShare = 226 * 1024 / kBlocks<NT> - kCapacity<DT, NT> * 8 - 5 * 1024;
+    plan.stash = (int)std::min<long long>(plan.slice_vectors / (NT * kBlockVectors), std::max(0, kShare) / (NT * kBlockVectors * 16));
+
     auto kernel = top_kernel<DT, NT>;
+    static PerDeviceOnce once;
     cudaLaunchConfig_t cfg = {};
     cfg.blockDim = dim3(NT);
     cfg.gridDim = dim3((unsigned)plan.cluster);
-    cfg.dynamicSmemBytes = kCapacity<DT, NT> * sizeof(unsigned long long);
+    cfg.dynamicSmemBytes = kCapacity<DT, NT> * sizeof(unsigned long long) + (size_t)plan.stash * NT * kBlockVectors * sizeof(uint4);
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = (unsigned)plan.cluster; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    cudaError_t e;
+    cudaError_t e = once.run([&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024); });
+    if (e != cudaSuccess) return e;
     // clusters that the device holds at once: asked again only when this thread's last answer was for another shape
-    static thread_local struct { int dev, cluster, clusters; } last = {-1, 0, 0};
+    static thread_local struct { int dev, cluster, clusters; size_t smem; } last = {-1, 0, 0, 0};
     int dev = 0;
     if ((e = cudaGetDevice(&dev)) != cudaSuccess) return e;
-    if (last.dev != dev || last.cluster != plan.cluster) {
+    if (last.dev != dev || last.cluster != plan.cluster || last.smem != cfg.dynamicSmemBytes) {
         int clusters = 0;
         if ((e = cudaOccupancyMaxActiveClusters(&clusters, kernel, &cfg)) != cudaSuccess) return e;
-        last = {dev, plan.cluster, clusters < 1 ? 1 : clusters};
+        last = {dev, plan.cluster, clusters < 1 ? 1 : clusters, cfg.dynamicSmemBytes};
     }
     cfg.gridDim = dim3((unsigned)(std::min<long long>(a.rows, last.clusters) * plan.cluster));
     return cudaLaunchKernelEx(&cfg, kernel, a, plan);
@@ -373,9 +429,10 @@ cudaError_t launch_top(const TopArgs& a, int dtype, int sms, cudaStream_t stream
     plan.cluster = 1;
     while (plan.cluster < kMaxCluster && a.rows * plan.cluster * 2 <= sms && vectors / plan.cluster > 256) plan.cluster *= 2;
     plan.slice_vectors = (vectors + plan.cluster - 1) / plan.cluster;
-    const bool small = vectors <= 1024 && a.rows > 2ll * sms;
-    if (dtype == kF32) return small ? launch_rows<kF32, 128>(a, plan, stream) : launch_rows<kF32, 256>(a, plan, stream);
-    return small ? launch_rows<kBF16, 128>(a, plan, stream) : launch_rows<kBF16, 256>(a, plan, stream);
+    int nt = vectors > 8192 ? 512 : vectors > 1024 || a.rows <= 2ll * sms ? 256 : 128;
+    if (const char* v = getenv("TM_TOP_NT")) nt = atoi(v);
+    if (dtype == kF32) return nt == 512 ? launch_rows<kF32, 512>(a, plan, stream) : nt == 128 ? launch_rows<kF32, 128>(a, plan, stream) : launch_rows<kF32, 256>(a, plan, stream);
+    return nt == 512 ? launch_rows<kBF16, 512>(a, plan, stream) : nt == 128 ? launch_rows<kBF16, 128>(a, plan, stream) : launch_rows<kBF16, 256>(a, plan, stream);
 }
 
 }  // namespace tmask
