@@ -9,6 +9,7 @@
 // digits where the student puts nearly everything on the list.  Terms with p = 0 are left out, and so is the rest's term where
 // the student has no mass there.
 #include <algorithm>
+#include <type_traits>
 
 #include "tm_launch.h"
 #include "tm_rows.cuh"
@@ -201,14 +202,17 @@ struct RowPlan {
     int cluster, slots;            // slots: list entries, a multiple of 32
     int slice_vectors, flags;      // flags: bytes, a multiple of 16 (0 without a loss)
     int stash;                     // blocks of NT * U vectors that stay in shared memory between the passes
-    double kappa;                  // (log2(e) / T) / c2, the rounding of c2
+    float inv_t, inv_t_low, c2;    // 1 / T and what its rounding left out; log2(e) / T
+    double inv_t_d, kappa;         // 1 / T; (log2(e) / T) / c2, the rounding of c2
 };
 
 constexpr int kBlockVectors = 4;                   // vectors of a thread's block
-template <int NT> constexpr int kBlocks = NT >= 384 ? 2 : NT == 256 ? 3 : 6;   // blocks an SM: the registers they may use
+// Blocks an SM, that is the registers a thread may use: as many as do without spills in the loops (the loss of 2048 x 32001 fp32 takes
+// 65 us with three blocks of 256 threads and 67 with four, the gradient alone in bf16 58.7 and 54.4)
+template <bool LOSS, int NT> constexpr int kBlocks = NT == 512 ? 2 : NT == 256 ? (LOSS ? 3 : 4) : 8;
 
 template <int DT, bool LOSS, bool GRAD, int NT>
-__global__ void __launch_bounds__(NT + 32, kBlocks<NT>) distill_kernel(const DistillArgs a, const RowPlan plan) {
+__global__ void __launch_bounds__(NT + 32, kBlocks<LOSS, NT>) distill_kernel(const DistillArgs a, const RowPlan plan) {
     using T = typename RowType<DT>::T;
     constexpr int V = RowType<DT>::kVec, NW = NT / 32, U = kBlockVectors;
     extern __shared__ __align__(16) uint8_t dynamic[];
@@ -227,7 +231,7 @@ __global__ void __launch_bounds__(NT + 32, kBlocks<NT>) distill_kernel(const Dis
     const bool lister = warp == NW;
     const int C = plan.cluster, slots = plan.slots;
     const uint32_t rank = C > 1 ? cluster_rank() : 0u;
-    const float inv_t = 1.0f / a.temperature, c2 = (float)(kLog2eD / a.temperature);
+    const float inv_t = plan.inv_t, c2 = plan.c2;
     const long long step = gridDim.x / C;
     for (int i = tid; i < kHash; i += NT + 32) hash[i] = -1;
     for (int i = tid; i < plan.flags / 16; i += NT + 32) reinterpret_cast<uint4*>(flags)[i] = make_uint4(0u, 0u, 0u, 0u);
@@ -293,7 +297,7 @@ __global__ void __launch_bounds__(NT + 32, kBlocks<NT>) distill_kernel(const Dis
             some = __any_sync(0xFFFFFFFFu, some) && weight != 0.0f;
             if (lane == 0) on_s = some;
             if (!LOSS) {
-                list.probabilities(a, weight, a.teacher_lse ? a.teacher_lse[r] : 0.0f, inv_t, (float)(1.0 / (double)a.temperature - (double)inv_t));
+                list.probabilities(a, weight, a.teacher_lse ? a.teacher_lse[r] : 0.0f, inv_t, plan.inv_t_low);
                 if (lane == 0) rest_s = list.rest;
 #pragma unroll
                 for (int e = 0; e < kEntries; ++e)
@@ -426,7 +430,7 @@ __global__ void __launch_bounds__(NT + 32, kBlocks<NT>) distill_kernel(const Dis
             if (lister) {
                 List list;
                 list.load(list_id, list_v, slots);
-                list.probabilities(a, weight, a.teacher_lse ? a.teacher_lse[r] : 0.0f, inv_t, (float)(1.0 / (double)a.temperature - (double)inv_t));
+                list.probabilities(a, weight, a.teacher_lse ? a.teacher_lse[r] : 0.0f, inv_t, plan.inv_t_low);
                 entropy = list.entropy; mass = list.mass; norm = list.norm;
                 float z[kEntries];
 #pragma unroll
@@ -506,8 +510,7 @@ __global__ void __launch_bounds__(NT + 32, kBlocks<NT>) distill_kernel(const Dis
             }
             if (lister && rank == 0) {
                 float lse, log_rest;
-                const double inv_t_d = 1.0 / (double)a.temperature;
-                const float loss = row_loss(entropy, mass, norm, rest, dot, inv_t_d, k.slow ? k.R * inv_t_d : k.R * plan.kappa * kLn2D, s_all, s_rest, lse, log_rest);
+                const float loss = row_loss(entropy, mass, norm, rest, dot, plan.inv_t_d, k.slow ? k.R * plan.inv_t_d : k.R * plan.kappa * kLn2D, s_all, s_rest, lse, log_rest);
                 if (lane == 0) {
                     a.loss[r] = loss * weight * a.scale;
                     if (!GRAD && a.stats) { a.stats[2 * r] = lse; a.stats[2 * r + 1] = a.teacher_lse ? log_rest : 0.0f; }
@@ -584,9 +587,9 @@ template <int DT, bool LOSS, bool GRAD, int NT> cudaError_t launch_rows(const Di
 }
 
 template <int DT, bool LOSS, bool GRAD, int NT> cudaError_t launch_as(const DistillArgs& a, RowPlan plan, cudaStream_t stream) {
-    // A third of an SM's shared memory for the stash, the least that three blocks leave each other
-    constexpr int kBlockBytes = NT * kBlockVectors * 16, kStashBytes = 64 * 1024;
-    plan.stash = LOSS && GRAD ? std::max(0, std::min(plan.slice_vectors / (NT * kBlockVectors), (kStashBytes - plan.flags) / kBlockBytes)) : 0;
+    // a block's share of an SM's 228 KB for the stash, less its flags and static arrays
+    constexpr int kBlockBytes = NT * kBlockVectors * 16, kShare = 226 * 1024 / kBlocks<LOSS, NT> - 9 * 1024;
+    plan.stash = LOSS && GRAD ? std::max(0, std::min(plan.slice_vectors / (NT * kBlockVectors), (kShare - plan.flags) / kBlockBytes)) : 0;
     return launch_rows<DT, LOSS, GRAD, NT>(a, plan, stream);
 }
 
@@ -595,7 +598,11 @@ template <bool LOSS, bool GRAD> cudaError_t launch(const DistillArgs& a, int dty
     const long long vectors = std::max<long long>(1, (a.vocab + 2 * V - 2) / V);      // of a row, wherever it starts
     RowPlan plan;
     plan.slots = (a.k + 31) / 32 * 32;
-    plan.kappa = kLog2eD / a.temperature / (double)(float)(kLog2eD / a.temperature);
+    plan.inv_t_d = 1.0 / (double)a.temperature;
+    plan.inv_t = (float)plan.inv_t_d;
+    plan.inv_t_low = (float)(plan.inv_t_d - (double)plan.inv_t);
+    plan.c2 = (float)(kLog2eD / a.temperature);
+    plan.kappa = kLog2eD / a.temperature / (double)plan.c2;
     // Several blocks to a row where the rows alone do not fill the device (a row of 131072 bf16 logits: 14 us on one block, 11.4 us on
     // eight), and where a row is longer than 256 KB
     plan.cluster = 1;
@@ -603,11 +610,16 @@ template <bool LOSS, bool GRAD> cudaError_t launch(const DistillArgs& a, int dty
     while (plan.cluster < kMaxCluster && a.rows * plan.cluster * 2 <= sms && vectors / plan.cluster > 256) plan.cluster *= 2;
     plan.slice_vectors = (int)((vectors + plan.cluster - 1) / plan.cluster);
     plan.flags = LOSS ? (plan.slice_vectors + 15) / 16 * 16 : 0;
-    // Short rows by small blocks, of which more are under way (4096 x 4000 fp32, loss and gradient: 63 us with 128 threads, 91 with 256);
-    // long ones by larger blocks, with more loads in flight than rows (300 x 32001 fp32: 28 and 24 us)
-    const bool small = vectors <= 2048 && a.rows > 2ll * sms;
-    if (dtype == kF32) return small ? launch_as<kF32, LOSS, GRAD, 128>(a, plan, stream) : launch_as<kF32, LOSS, GRAD, 256>(a, plan, stream);
-    return small ? launch_as<kBF16, LOSS, GRAD, 128>(a, plan, stream) : launch_as<kBF16, LOSS, GRAD, 256>(a, plan, stream);
+    // Short rows by small blocks, of which more are under way (4096 x 4000 fp32, loss and gradient: 50 us with 128 threads, 75 with 256);
+    // longer ones by larger blocks, with more loads in flight than rows (300 x 32001 fp32: 32 and 24 us); the longest, where the
+    // gradient reads them again, by fewer and larger blocks, whose rows then fit L2 (4096 x 131072 bf16: 505 us with 256, 453 with 512)
+    auto as = [&](auto type) {
+        constexpr int DT = decltype(type)::value;
+        if (vectors <= 2048 && a.rows > 2ll * sms) return launch_as<DT, LOSS, GRAD, 128>(a, plan, stream);
+        if constexpr (LOSS && GRAD) { if (vectors > 8192) return launch_as<DT, LOSS, GRAD, 512>(a, plan, stream); }
+        return launch_as<DT, LOSS, GRAD, 256>(a, plan, stream);
+    };
+    return dtype == kF32 ? as(std::integral_constant<int, kF32>()) : as(std::integral_constant<int, kBF16>());
 }
 
 }  // namespace

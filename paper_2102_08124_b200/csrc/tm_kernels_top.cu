@@ -11,7 +11,6 @@
 // Where far more reach the bound than the buffer holds (few threads have seen all the large ones), the vectors are gone through
 // again one of each thread at a time, a radix selection cutting the buffer back to k, and raising the bound, whenever it fills up.
 #include <algorithm>
-#include <cstdlib>
 
 #include "tm_launch.h"
 #include "tm_rows.cuh"
@@ -429,8 +428,9 @@ cudaError_t launch_top(const TopArgs& a, int dtype, int sms, cudaStream_t stream
     plan.cluster = 1;
     while (plan.cluster < kMaxCluster && a.rows * plan.cluster * 2 <= sms && vectors / plan.cluster > 256) plan.cluster *= 2;
     plan.slice_vectors = (vectors + plan.cluster - 1) / plan.cluster;
-    int nt = vectors > 8192 ? 512 : vectors > 1024 || a.rows <= 2ll * sms ? 256 : 128;
-    if (const char* v = getenv("TM_TOP_NT")) nt = atoi(v);
+    // Short rows by small blocks, of which more are under way (4096 x 1000 bf16: 25 us with 128 threads, 44 with 256); the longest by
+    // large ones, whose rows then fit L2 (4096 x 131072 bf16: 335 us with 256, 333 with 512; 64 x 100000: 17.7 and 14.8)
+    const int nt = vectors > 8192 ? 512 : vectors > 1024 || a.rows <= 2ll * sms ? 256 : 128;
     if (dtype == kF32) return nt == 512 ? launch_rows<kF32, 512>(a, plan, stream) : nt == 128 ? launch_rows<kF32, 128>(a, plan, stream) : launch_rows<kF32, 256>(a, plan, stream);
     return nt == 512 ? launch_rows<kBF16, 512>(a, plan, stream) : nt == 128 ? launch_rows<kBF16, 128>(a, plan, stream) : launch_rows<kBF16, 256>(a, plan, stream);
 }
