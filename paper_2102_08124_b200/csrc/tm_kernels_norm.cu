@@ -4,50 +4,117 @@
 //   backward   g = dy w;  xh = (h - mu) r;  dx = r (g - mean_c g - xh mean_c (g xh)) (+ dsum);
 //              dw = sum_rows dy xh;  db = sum_rows dy
 //
-// Bound: HBM (8 respectively 14 operations an element against 4 to 16 bytes).  A row is read once and stays in the registers of
-// the threads that share it -- 8 or 32 threads of a warp, or a whole CTA, by its width -- between the reductions and the
-// output, so nothing is read twice and the centred squares are summed after the mean is known (no difference of large
-// numbers).  The normalised value uses the sum before it is rounded for sum_out: one rounding, at the end.
+// Bound: HBM by bytes (8 respectively 14 operations an element against 4 to 16 bytes); as measured the latency of a row's loads and
+// reductions, after the number of instructions was halved (backward, 16384 x 1024 bf16: from 25.0 to 13.3 million warp instructions): two
+// elements an instruction wherever there is a packed form, parameters in registers over all rows, nothing worked out twice.
+// A row belongs to a group of threads -- 8 or 32 of a warp, or up to 1024, by its width -- and stays in their registers between the
+// reductions and the output: it is read once.  Groups go through the rows with a stride and ask for the next row before they
+// reduce this one; several groups an SM cover each other's latency.
+// Measured, copy bandwidth 6.55 TB/s: forward with residual and sum 16384 x 1024 bf16 29.6 us (4.5 TB/s), 8000 x 4096 bf16 27.6 us
+// (4.8), 4097 x 1001 fp32 11.9 us; backward 16384 x 1024 bf16 with dsum 32.7 us (4.1), fp32 38.7 us (5.2), 2047 x 8191 bf16 63 us.
+// The centred squares are summed after the mean is known (no difference of large numbers); the normalised value uses the sum
+// before it is rounded for sum_out: one rounding, at the end.
 // A thread owns the same columns of every row, so the backward pass keeps its share of dw and db in registers over all rows
-// that its CTA takes; CTAs leave one partial row each, which a second kernel adds up in a fixed order (same input, same bits).
-// Rows wider than the register forms read the row again from L2 for every step (wide_* kernels).
+// that its block takes; blocks leave one partial row each, which a second kernel adds up in a fixed order (same input, same bits).
+// The backward pass of rows too wide for that reads them from a ring of stages in shared memory that bulk copies fill (ring kernel);
+// rows wider still are read again from L2 for every step (wide_* kernels).
 #include <algorithm>
+#include <type_traits>
 
 #include "tm_launch.h"
 #include "tm_rows.cuh"
+#include "tm_tma.cuh"
 
 namespace tmask {
 
+// Partial rows of the parameters' gradients, one a block of the backward kernel: as many as the device holds, up to the memory that
+// they are worth.
+int norm_partial_rows(long long rows, long long cols) {
+    const long long cap = cols <= 4096 ? 888 : (cols <= 65536 ? 296 : 64);
+    return (int)std::max<long long>(1, std::min(rows, cap));
+}
+
 namespace {
 
-// VB consecutive bytes of a row as one access, kept as stored until used
+constexpr int kMaxStages = 4, kMaxGroups = 16, kMaxStreams = 3;
+
+// The rows of one input matrix as they are copied: [begin, end) is the memory that the matrix covers, first to last element.
+struct Stream {
+    const char *begin, *end;
+    long long pitch;               // bytes
+};
+// A row in a stage: the bytes [lo, hi) that are copied, rounded outwards to 16-byte boundaries where that stays inside the matrix, else
+// inwards (only its first and last row can be so).
+struct RowBytes {
+    const char *start, *lo;
+    uint32_t bytes;
+    __device__ __forceinline__ RowBytes(const Stream& m, long long r, uint32_t row_bytes) {
+        start = m.begin + r * m.pitch;
+        const char* down = reinterpret_cast<const char*>(reinterpret_cast<uintptr_t>(start) & ~(uintptr_t)15);
+        const char* up = reinterpret_cast<const char*>((reinterpret_cast<uintptr_t>(start) + row_bytes + 15) & ~(uintptr_t)15);
+        lo = down < m.begin ? down + 16 : down;
+        if (up > m.end) up -= 16;
+        bytes = up > lo ? (uint32_t)(up - lo) : 0u;
+    }
+};
+struct RingPlan {
+    int groups, stages, streams;
+    uint32_t row_bytes, stage_bytes;           // of one stream: a row, a stage
+    Stream in[kMaxStreams];
+};
+
+// VB bytes of a row: N elements from column c on, out of a stage or from the row itself
 template <int DT, int VB> struct Access {
+    using T = typename RowType<DT>::T;
     static constexpr int kElems = VB / RowType<DT>::kBytes;
-    static constexpr int kWords = VB >= 4 ? VB / 4 : 1;
-    uint32_t w[kWords];
-    __device__ __forceinline__ void load(const void* p) {
+    static __device__ __forceinline__ void load(const char* p, float* v) {
+        if constexpr (VB == 16) unpack_vector<DT>(*reinterpret_cast<const uint4*>(p), v);
+        else v[0] = to_float(*reinterpret_cast<const T*>(p));
+    }
+    static __device__ __forceinline__ void store(T* p, const float* v) {
         if constexpr (VB == 16) {
-            const uint4 u = *static_cast<const uint4*>(p);
-            w[0] = u.x; w[1] = u.y; w[2] = u.z; w[3] = u.w;
-        } else if constexpr (VB == 4) w[0] = *static_cast<const uint32_t*>(p);
-        else w[0] = *static_cast<const uint16_t*>(p);
+            uint32_t o[4];
+            pack_words<DT, 4>(v, o);
+            *reinterpret_cast<uint4*>(p) = make_uint4(o[0], o[1], o[2], o[3]);
+        } else from_float(p, v[0]);
     }
-    __device__ __forceinline__ void clear() {
-#pragma unroll
-        for (int i = 0; i < kWords; ++i) w[i] = 0u;
-    }
-    __device__ __forceinline__ float get(int j) const {
-        if constexpr (DT == kF32) return __uint_as_float(w[j]);
-        else return (j & 1) ? __uint_as_float(w[j >> 1] & 0xFFFF0000u) : __uint_as_float(w[j >> 1] << 16);
-    }
-    static __device__ __forceinline__ void store(void* p, const float* v) {
-        if constexpr (VB == 2) *static_cast<__nv_bfloat16*>(p) = __float2bfloat16_rn(v[0]);
-        else {
-            uint32_t o[kWords];
-            pack_words<DT, kWords>(v, o);
-            if constexpr (VB == 16) *static_cast<uint4*>(p) = make_uint4(o[0], o[1], o[2], o[3]);
-            else *static_cast<uint32_t*>(p) = o[0];
+};
+
+// A group's ring: rows n = 0, 1, ... of the group go through its stages in turn.
+struct GroupRing {
+    const RingPlan& plan;
+    char* stage0;
+    uint64_t* bars;
+    __device__ __forceinline__ char* stage(int slot, int stream) const { return stage0 + (size_t)(slot * plan.streams + stream) * plan.stage_bytes; }
+    // one thread: asks for a row
+    __device__ __forceinline__ void ask(int slot, long long r) const {
+        uint32_t all = 0;
+        for (int k = 0; k < plan.streams; ++k) all += RowBytes(plan.in[k], r, plan.row_bytes).bytes;
+        fence_proxy_async_smem();
+        mbar_expect_tx(bars + slot, all);
+        for (int k = 0; k < plan.streams; ++k) {
+            const RowBytes b(plan.in[k], r, plan.row_bytes);
+            if (b.bytes) asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                                      ::"r"(smem_addr(stage(slot, k))), "l"(b.lo), "r"(b.bytes), "r"(smem_addr(bars + slot)) : "memory");
         }
+    }
+};
+// A stream's row in its stage: elements by column.  Those that the copy left out (at most 7 at either end of the matrix) come from the row.
+template <int DT, int VB> struct RowInStage {
+    const char *start, *copy;      // the row, and where it would start in the stage
+    int from, to;                  // columns that are in the stage
+    __device__ __forceinline__ RowInStage(const Stream& m, long long r, uint32_t row_bytes, const char* stage) {
+        const RowBytes b(m, r, row_bytes);
+        constexpr int B = RowType<DT>::kBytes;
+        start = b.start;
+        copy = stage + (b.start - b.lo);
+        from = b.lo > b.start ? (int)((b.lo - b.start) / B) : 0;
+        to = min((int)(row_bytes / B), (int)((b.lo + b.bytes - b.start) / B));
+    }
+    __device__ __forceinline__ void load(int c, float* v) const {
+        const char* p = copy + (long long)c * RowType<DT>::kBytes;
+        if constexpr (VB != 16) { if (c < from || c >= to) p = start + (long long)c * RowType<DT>::kBytes; }
+        Access<DT, VB>::load(p, v);
     }
 };
 
@@ -84,6 +151,8 @@ template <int N> __device__ __forceinline__ void load_params(const void* p, bool
     }
 }
 
+constexpr long long kRingWidth = 16384;
+
 template <int DT> __device__ __forceinline__ const typename RowType<DT>::T* row_of(const void* p, long long ld, long long r) {
     return static_cast<const typename RowType<DT>::T*>(p) + r * ld;
 }
@@ -91,74 +160,149 @@ template <int DT> __device__ __forceinline__ typename RowType<DT>::T* row_of(voi
     return static_cast<typename RowType<DT>::T*>(p) + r * ld;
 }
 
-// TPR threads share a row, E elements each in accesses of VB bytes; access i of thread t starts at column (i TPR + t) VB / size
-template <int DT, int VB, int TPR, int E>
-__global__ void __launch_bounds__(TPR <= 32 ? 128 : TPR) norm_forward_kernel(const NormArgs a) {
+// Sets a block's rings up and starts them; returns this group's.
+template <int TPR> __device__ __forceinline__ GroupRing start_ring(const RingPlan& plan, char* smem, uint64_t* bars, long long first, long long step, long long rows) {
+    const int g = threadIdx.x / TPR, S = plan.stages;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < plan.groups * S; ++i) mbar_init(bars + i, 1);
+        fence_mbar_init();
+    }
+    __syncthreads();
+    const GroupRing ring{plan, smem + (size_t)g * S * plan.streams * plan.stage_bytes, bars + g * S};
+    if (threadIdx.x % TPR == 0)
+        for (int k = 0; k < S; ++k) { const long long r = first + k * step; if (r < rows) ring.ask(k, r); }
+    return ring;
+}
+
+// Threads of a block whose rows are shared by TPR threads each, and blocks an SM (the registers they may use).  Backward: a block
+// leaves one partial row of parameter gradients, so the groups of rows up to 2048 columns share larger blocks.
+template <int TPR> constexpr int kForwardThreads = TPR <= 32 ? 128 : TPR;
+template <int TPR, int E> constexpr int kBackwardThreads = TPR <= 32 ? 128 : TPR <= 128 ? 384 : TPR <= 256 ? (E <= 8 ? 768 : 256) : TPR;
+template <int TPR, int E> constexpr int kForwardBlocks = std::max(1, (E <= 8 ? 1024 : 768) / kForwardThreads<TPR>);
+template <int TPR, int E> constexpr int kBackwardBlocks = std::max(1, (E <= 8 ? 768 : 512) / kBackwardThreads<TPR, E>);
+
+// What TPR threads hold of a row: E elements each, in accesses of VB bytes; access i of thread t starts at column (i TPR + t) VB / size.
+template <int DT, int VB, int TPR, int E> struct RowRegs {
     using A = Access<DT, VB>;
-    constexpr int VE = A::kElems, NV = E / VE, kThreads = TPR <= 32 ? 128 : TPR, kGroups = kThreads / TPR;
-    __shared__ float buf[2][32];
-    const int t = threadIdx.x % TPR, g = threadIdx.x / TPR;
-    const float inv_n = 1.0f / (float)a.cols;
-    for (long long r0 = (long long)blockIdx.x * kGroups; r0 < a.rows; r0 += (long long)gridDim.x * kGroups) {
-        const long long r = r0 + g;
-        const bool on = r < a.rows;                       // whole groups idle together, but take part in the shuffles
-        float h[E];
-        {
-            A x[NV];
-            const auto* xr = row_of<DT>(a.x, a.ld_x, on ? r : 0);
-#pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const long long c = (long long)(i * TPR + t) * VE;
-                if (on && c < a.cols) x[i].load(xr + c); else x[i].clear();
-            }
-            if (a.residual) {
-                A s[NV];
-                const auto* sr = row_of<DT>(a.residual, a.ld_residual, on ? r : 0);
-#pragma unroll
-                for (int i = 0; i < NV; ++i) {
-                    const long long c = (long long)(i * TPR + t) * VE;
-                    if (on && c < a.cols) s[i].load(sr + c); else s[i].clear();
-                }
-#pragma unroll
-                for (int k = 0; k < E; ++k) h[k] = x[k / VE].get(k % VE) + s[k / VE].get(k % VE);
-            } else {
-#pragma unroll
-                for (int k = 0; k < E; ++k) h[k] = x[k / VE].get(k % VE);
-            }
-        }
-        float sum = 0.0f;
-#pragma unroll
-        for (int k = 0; k < E; ++k) sum += h[k];
-        const float mean = row_sum<TPR>(sum, buf[0]) * inv_n;
-        float sq = 0.0f;
+    using T = typename RowType<DT>::T;
+    static constexpr int VE = A::kElems, NV = E / VE;
+    static __device__ __forceinline__ int column(int i) { return (i * TPR + (int)threadIdx.x % TPR) * VE; }
+    // (v, v) for elements 2k and 2k + 1, zero for those past the last column
+    static __device__ __forceinline__ float2 inside(int k, int cols, float v) {
+        return make_float2(column(2 * k / VE) < cols ? v : 0.0f, column((2 * k + 1) / VE) < cols ? v : 0.0f);
+    }
+    static __device__ __forceinline__ void load(const T* row, int cols, float2 (&v)[E / 2]) {
+        float* f = reinterpret_cast<float*>(v);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            if ((long long)(i * TPR + t) * VE < a.cols) {
+            const int c = column(i);
 #pragma unroll
-                for (int j = 0; j < VE; ++j) { const float d = h[i * VE + j] - mean; sq = fmaf(d, d, sq); }
-            }
+            for (int j = 0; j < VE; ++j) f[i * VE + j] = 0.0f;
+            if (c < cols) A::load(reinterpret_cast<const char*>(row + c), f + i * VE);
         }
-        const float rstd = rsqrtf(row_sum<TPR>(sq, buf[1]) * inv_n + a.eps);
+    }
+    // the same in two steps, for a row that is asked for ahead of its turn
+    using Raw = std::conditional_t<VB == 16, uint4, T>;
+    static __device__ __forceinline__ void ask(const T* row, int cols, Raw (&u)[NV]) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            u[i] = Raw{};
+            if (column(i) < cols) u[i] = *reinterpret_cast<const Raw*>(row + column(i));
+        }
+    }
+    static __device__ __forceinline__ void take(const Raw (&u)[NV], float2 (&v)[E / 2]) {
+        float* f = reinterpret_cast<float*>(v);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            if constexpr (VB == 16) unpack_vector<DT>(u[i], f + i * VE);
+            else f[i] = to_float(u[i]);
+        }
+    }
+    static __device__ __forceinline__ void store(T* row, int cols, const float2 (&v)[E / 2]) {
+        const float* f = reinterpret_cast<const float*>(v);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = column(i);
+            if (c < cols) A::store(row + c, f + i * VE);
+        }
+    }
+    static __device__ __forceinline__ void params(const void* p, bool f32, bool vec, int cols, float2 (&v)[E / 2], float none) {
+        float* f = reinterpret_cast<float*>(v);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = column(i);
+#pragma unroll
+            for (int j = 0; j < VE; ++j) f[i * VE + j] = 0.0f;
+            if (c < cols) load_params<VE>(p, f32, vec, c, f + i * VE, none);
+        }
+    }
+};
+
+template <int DT, int VB, int TPR, int E>
+__global__ void __launch_bounds__(kForwardThreads<TPR>, kForwardBlocks<TPR, E>) norm_forward_kernel(const NormArgs a) {
+    using R = RowRegs<DT, VB, TPR, E>;
+    constexpr int P = E / 2, kGroups = kForwardThreads<TPR> / TPR;
+    // kAhead: the next row is asked for before this one is reduced, where the registers suffice.  Without and with, us: 16384 x 1024
+    // bf16 50.2 and 29.6, 32768 x 512 bf16 21.5 and 15.4, 8000 x 4096 bf16 35.7 and 27.6, 2047 x 8191 bf16 41.9 and 26.3; where they
+    // do not (8 elements in accesses of one, fp32) 4097 x 1001 13.9 and 15.7.  kKeep: weight and bias stay in registers over all rows.
+    constexpr bool kAhead = VB == 16 ? DT == kBF16 || R::NV <= 2 : E == 16 && (TPR == 256 || TPR == 512), kKeep = E < 32;
+    __shared__ float buf[2][32];
+    const int t = threadIdx.x % TPR, g = threadIdx.x / TPR, cols = (int)a.cols;
+    const float inv_n = 1.0f / (float)a.cols;
+    const long long step = (long long)gridDim.x * kGroups;
+    float2 w[P], b[P];
+    if constexpr (kKeep) {
+        R::params(a.weight, a.weight_f32, a.weight_vec, cols, w, 1.0f);
+        R::params(a.bias, a.weight_f32, a.bias_vec, cols, b, 0.0f);
+    }
+    typename R::Raw ux[R::NV], us[R::NV];
+    const auto ask = [&](long long r) {
+        if constexpr (kAhead) {
+            const int n = r < a.rows ? cols : 0;
+            R::ask(row_of<DT>(a.x, a.ld_x, r), n, ux);
+            if (a.residual) R::ask(row_of<DT>(a.residual, a.ld_residual, r), n, us);
+        }
+    };
+    ask((long long)blockIdx.x * kGroups + g);
+    for (long long r0 = (long long)blockIdx.x * kGroups; r0 < a.rows; r0 += step) {
+        const long long r = r0 + g;
+        const bool on = r < a.rows;                       // whole groups idle together, but take part in the shuffles and barriers
+        float2 h[P];
+        if constexpr (kAhead) R::take(ux, h);
+        else R::load(row_of<DT>(a.x, a.ld_x, r), on ? cols : 0, h);
+        if (a.residual) {
+            float2 s[P];
+            if constexpr (kAhead) R::take(us, s);
+            else R::load(row_of<DT>(a.residual, a.ld_residual, r), on ? cols : 0, s);
+#pragma unroll
+            for (int k = 0; k < P; ++k) h[k] = __fadd2_rn(h[k], s[k]);
+        }
+        ask(r + step);
+        if (a.sum && on) R::store(row_of<DT>(a.sum, a.ld_sum, r), cols, h);
+        float2 add = h[0];
+#pragma unroll
+        for (int k = 1; k < P; ++k) add = __fadd2_rn(add, h[k]);
+        const float mean = row_sum<TPR>(add.x + add.y, buf[0]) * inv_n;
+        float2 sq = make_float2(0.0f, 0.0f);
+#pragma unroll
+        for (int k = 0; k < P; ++k) {
+            h[k] = __fadd2_rn(h[k], R::inside(k, cols, -mean));      // the zeros past the last column stay zeros
+            sq = __ffma2_rn(h[k], h[k], sq);
+        }
+        const float rstd = rsqrtf(row_sum<TPR>(sq.x + sq.y, buf[1]) * inv_n + a.eps);
         if (!on) continue;
         if (t == 0) {
             if (a.mean) a.mean[r] = mean;
             if (a.rstd) a.rstd[r] = rstd;
         }
-        auto* yr = row_of<DT>(a.y, a.ld_y, r);
-        auto* hr = a.sum ? row_of<DT>(a.sum, a.ld_sum, r) : nullptr;
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const long long c = (long long)(i * TPR + t) * VE;
-            if (c < a.cols) {
-                float w[VE], b[VE], o[VE];
-                load_params<VE>(a.weight, a.weight_f32, a.weight_vec, c, w, 1.0f);
-                load_params<VE>(a.bias, a.weight_f32, a.bias_vec, c, b, 0.0f);
-#pragma unroll
-                for (int j = 0; j < VE; ++j) o[j] = fmaf((h[i * VE + j] - mean) * rstd, w[j], b[j]);
-                A::store(yr + c, o);
-                if (hr) A::store(hr + c, h + i * VE);
-            }
+        if constexpr (!kKeep) {
+            R::params(a.weight, a.weight_f32, a.weight_vec, cols, w, 1.0f);
+            R::params(a.bias, a.weight_f32, a.bias_vec, cols, b, 0.0f);
         }
+        const float2 rr = make_float2(rstd, rstd);
+#pragma unroll
+        for (int k = 0; k < P; ++k) h[k] = __ffma2_rn(__fmul2_rn(h[k], rr), w[k], b[k]);
+        R::store(row_of<DT>(a.y, a.ld_y, r), cols, h);
     }
 }
 
@@ -193,96 +337,189 @@ template <int DT> __global__ void __launch_bounds__(1024) wide_norm_forward_kern
 }
 
 template <int DT, int VB, int TPR, int E>
-__global__ void __launch_bounds__(TPR <= 32 ? 128 : TPR) norm_backward_kernel(const NormBackArgs a) {
-    using A = Access<DT, VB>;
-    constexpr int VE = A::kElems, NV = E / VE, kThreads = TPR <= 32 ? 128 : TPR, kGroups = kThreads / TPR;
-    __shared__ float buf[4][32];
+__global__ void __launch_bounds__(kBackwardThreads<TPR, E>, kBackwardBlocks<TPR, E>) norm_backward_kernel(const NormBackArgs a) {
+    using R = RowRegs<DT, VB, TPR, E>;
+    constexpr int P = E / 2, kThreads = kBackwardThreads<TPR, E>, kGroups = kThreads / TPR;
+    // As in the forward kernel.  Without and with asking ahead, us: 16384 x 1024 bf16 38.3 and 32.7; fp32 spills: 30000 x 100 20.1
+    // and 26.2.
+    constexpr bool kAhead = VB == 16 && DT == kBF16, kKeep = TPR < 1024;
+    __shared__ float2 buf[2][32];
     extern __shared__ float fold[];                       // kGroups > 1: [2][cols]
-    const int t = threadIdx.x % TPR, g = threadIdx.x / TPR;
+    const int g = threadIdx.x / TPR, cols = (int)a.cols;
     const float inv_n = 1.0f / (float)a.cols;
+    const long long step = (long long)gridDim.x * kGroups;
+    float2 w[P], dw[P], db[P];
+    if constexpr (kKeep) R::params(a.weight, a.weight_f32, a.weight_vec, cols, w, 1.0f);
+#pragma unroll
+    for (int k = 0; k < P; ++k) dw[k] = db[k] = make_float2(0.0f, 0.0f);
+    int turn = 0;
+    typename R::Raw ud[R::NV], ux[R::NV], ue[R::NV];
+    float next_mean = 0.0f, next_rstd = 0.0f;
+    const auto ask = [&](long long r) {
+        if constexpr (kAhead) {
+            const bool on = r < a.rows;
+            R::ask(row_of<DT>(a.dy, a.ld_dy, r), on ? cols : 0, ud);
+            R::ask(row_of<DT>(a.h, a.ld_h, r), on ? cols : 0, ux);
+            R::ask(row_of<DT>(a.dsum, a.ld_dsum, r), on && a.dsum ? cols : 0, ue);
+            next_mean = on ? a.mean[r] : 0.0f;
+            next_rstd = on ? a.rstd[r] : 0.0f;
+        }
+    };
+    ask((long long)blockIdx.x * kGroups + g);
+    for (long long r0 = (long long)blockIdx.x * kGroups; r0 < a.rows; r0 += step, turn ^= 1) {
+        const long long r = r0 + g;
+        const bool on = r < a.rows;
+        float2 d[P], x[P], e[P];
+        float mean, rstd;
+        if constexpr (kAhead) {
+            R::take(ud, d);
+            R::take(ux, x);
+            R::take(ue, e);                               // zeros without a dsum
+            mean = next_mean;
+            rstd = next_rstd;
+        } else {
+            R::load(row_of<DT>(a.dy, a.ld_dy, r), on ? cols : 0, d);
+            R::load(row_of<DT>(a.h, a.ld_h, r), on ? cols : 0, x);
+            mean = on ? a.mean[r] : 0.0f;
+            rstd = on ? a.rstd[r] : 0.0f;
+            R::load(row_of<DT>(a.dsum, a.ld_dsum, r), on && a.dsum ? cols : 0, e);
+        }
+        ask(r + step);
+        const float2 minus = make_float2(-mean, -mean), rs = make_float2(rstd, rstd);
+        if constexpr (!kKeep) R::params(a.weight, a.weight_f32, a.weight_vec, cols, w, 1.0f);
+        float2 s1 = make_float2(0.0f, 0.0f), s2 = s1;
+#pragma unroll
+        for (int k = 0; k < P; ++k) {
+            x[k] = __fmul2_rn(__fadd2_rn(x[k], minus), R::inside(k, cols, rstd));      // zero past the last column
+            dw[k] = __ffma2_rn(d[k], x[k], dw[k]);
+            db[k] = __fadd2_rn(db[k], d[k]);
+            d[k] = __fmul2_rn(d[k], w[k]);
+            s1 = __fadd2_rn(s1, d[k]);
+            s2 = __ffma2_rn(d[k], x[k], s2);
+        }
+        const float2 both = row_sum2<TPR>(make_float2(s1.x + s1.y, s2.x + s2.y), buf[turn]);
+        if (!on) continue;
+        const float m1 = -both.x * inv_n, m2 = -both.y * inv_n;
+        const float2 mm1 = make_float2(m1, m1), mm2 = make_float2(m2, m2);
+#pragma unroll
+        for (int k = 0; k < P; ++k) {
+            const float2 v = __fadd2_rn(__ffma2_rn(x[k], mm2, d[k]), mm1);
+            d[k] = __ffma2_rn(v, rs, e[k]);
+        }
+        R::store(row_of<DT>(a.dx, a.ld_dx, r), cols, d);
+    }
+    if (!a.partials) return;
+    float* out = a.partials + (long long)blockIdx.x * 2 * a.cols;
+    const float *fw = reinterpret_cast<const float*>(dw), *fb = reinterpret_cast<const float*>(db);
+    // the groups add their columns one after the other
+#pragma unroll 1
+    for (int k = 0; k < kGroups; ++k) {
+        if (kGroups > 1) __syncthreads();
+        if (g != k) continue;
+        float* to = k + 1 == kGroups ? out : fold;
+#pragma unroll
+        for (int q = 0; q < E; ++q) {
+            const int c = R::column(q / R::VE) + q % R::VE;
+            if (c < cols) {
+                to[c] = fw[q] + (k ? fold[c] : 0.0f);
+                to[cols + c] = fb[q] + (k ? fold[cols + c] : 0.0f);
+            }
+        }
+    }
+}
+
+// Rows of 8193 to kRingWidth columns: two rows' inputs do not fit the registers beside the parameters' gradients, so bulk copies bring the
+// next rows to shared memory.  2000 x 16384 bf16 87 us, 3000 x 9000 fp32 87 us; with every step read from L2 again 198 and 186 us.  For
+// narrower rows the registers are faster: 16384 x 1024 bf16 77 us by this kernel, 32.7 us by the one above.
+// streams: dy, h and, with a third one, dsum
+template <int DT, int VB, int TPR, int E>
+__global__ void __launch_bounds__(512, 1) ring_norm_backward_kernel(const __grid_constant__ NormBackArgs a, const __grid_constant__ RingPlan plan) {
+    using A = Access<DT, VB>;
+    constexpr int VE = A::kElems, NV = E / VE;
+    extern __shared__ __align__(128) char smem[];
+    __shared__ __align__(8) uint64_t bars[kMaxGroups * kMaxStages];
+    __shared__ float2 buf[2][32];
+    const int t = threadIdx.x % TPR, g = threadIdx.x / TPR, G = plan.groups, cols = (int)a.cols;
+    const float inv_n = 1.0f / (float)a.cols;
+    const long long first = (long long)blockIdx.x * G + g, step = (long long)gridDim.x * G;
+    const GroupRing ring = start_ring<TPR>(plan, smem, bars, first, step, a.rows);
     float dw[E], db[E];
 #pragma unroll
     for (int k = 0; k < E; ++k) dw[k] = db[k] = 0.0f;
-    int turn = 0;
-    for (long long r0 = (long long)blockIdx.x * kGroups; r0 < a.rows; r0 += (long long)gridDim.x * kGroups, turn ^= 2) {
-        const long long r = r0 + g;
-        const bool on = r < a.rows;
-        const long long rr = on ? r : 0;
-        A dy[NV], h[NV];
-        const auto* dyr = row_of<DT>(a.dy, a.ld_dy, rr);
-        const auto* hr = row_of<DT>(a.h, a.ld_h, rr);
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const long long c = (long long)(i * TPR + t) * VE;
-            if (on && c < a.cols) { dy[i].load(dyr + c); h[i].load(hr + c); } else { dy[i].clear(); h[i].clear(); }
-        }
-        const float mean = a.mean[rr], rstd = a.rstd[rr];
+    int slot = 0, turn = 0;
+    uint32_t phase = 0;
+    float next_mean = 0.0f, next_rstd = 0.0f;
+    if (first < a.rows) { next_mean = a.mean[first]; next_rstd = a.rstd[first]; }
+    for (long long r = first; r < a.rows; r += step, turn ^= 1) {
+        float mean = next_mean;
+        const float rstd = next_rstd;
+        if (r + step < a.rows) { next_mean = a.mean[r + step]; next_rstd = a.rstd[r + step]; }
+        if (!mbar_wait_bounded(ring.bars + slot, phase)) mean = __uint_as_float(0x7FC00000u);     // a row whose copy did not come in time shows as NaN
+        const RowInStage<DT, VB> dy(plan.in[0], r, plan.row_bytes, ring.stage(slot, 0)), h(plan.in[1], r, plan.row_bytes, ring.stage(slot, 1));
         float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const long long c = (long long)(i * TPR + t) * VE;
-            if (on && c < a.cols) {
-                float w[VE];
+            const int c = (i * TPR + t) * VE;
+            if (c < cols) {
+                float w[VE], d[VE], x[VE];
                 load_params<VE>(a.weight, a.weight_f32, a.weight_vec, c, w, 1.0f);
+                dy.load(c, d);
+                h.load(c, x);
 #pragma unroll
                 for (int j = 0; j < VE; ++j) {
-                    const float d = dy[i].get(j), xh = (h[i].get(j) - mean) * rstd, u = d * w[j];
+                    const float xh = (x[j] - mean) * rstd, u = d[j] * w[j];
                     s1 += u;
                     s2 = fmaf(u, xh, s2);
-                    dw[i * VE + j] = fmaf(d, xh, dw[i * VE + j]);
-                    db[i * VE + j] += d;
+                    dw[i * VE + j] = fmaf(d[j], xh, dw[i * VE + j]);
+                    db[i * VE + j] += d[j];
                 }
             }
         }
-        s1 = row_sum<TPR>(s1, buf[turn]) * inv_n;
-        s2 = row_sum<TPR>(s2, buf[turn + 1]) * inv_n;
-        if (!on) continue;
+        const float2 both = row_sum2<TPR>(make_float2(s1, s2), buf[turn]);
+        s1 = both.x * inv_n;
+        s2 = both.y * inv_n;
         auto* dxr = row_of<DT>(a.dx, a.ld_dx, r);
-        const auto* er = a.dsum ? row_of<DT>(a.dsum, a.ld_dsum, r) : nullptr;
+        const RowInStage<DT, VB> e(plan.in[plan.streams - 1], r, plan.row_bytes, ring.stage(slot, plan.streams - 1));
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const long long c = (long long)(i * TPR + t) * VE;
-            if (c < a.cols) {
-                float w[VE], o[VE];
+            const int c = (i * TPR + t) * VE;
+            if (c < cols) {
+                float w[VE], d[VE], x[VE], o[VE];
                 load_params<VE>(a.weight, a.weight_f32, a.weight_vec, c, w, 1.0f);
-                A e;
-                if (er) e.load(er + c); else e.clear();
+                dy.load(c, d);
+                h.load(c, x);
 #pragma unroll
-                for (int j = 0; j < VE; ++j) {
-                    const float xh = (h[i].get(j) - mean) * rstd;
-                    o[j] = fmaf(rstd, dy[i].get(j) * w[j] - s1 - xh * s2, e.get(j));
+                for (int j = 0; j < VE; ++j) o[j] = rstd * (d[j] * w[j] - s1 - (x[j] - mean) * rstd * s2);
+                if (plan.streams > 2) {
+                    float v[VE];
+                    e.load(c, v);
+#pragma unroll
+                    for (int j = 0; j < VE; ++j) o[j] += v[j];
                 }
                 A::store(dxr + c, o);
             }
         }
+        row_barrier<TPR>();
+        if (t == 0 && r + plan.stages * step < a.rows) ring.ask(slot, r + plan.stages * step);
+        if (++slot == plan.stages) { slot = 0; phase ^= 1u; }
     }
     if (!a.partials) return;
+    // the groups add their columns one after the other; the rings are done with
     float* out = a.partials + (long long)blockIdx.x * 2 * a.cols;
-    if constexpr (kGroups > 1) {
-        // the groups add their columns one after the other
-        for (int k = 0; k < kGroups; ++k) {
-            if (g == k) {
-#pragma unroll
-                for (int i = 0; i < NV; ++i)
-#pragma unroll
-                    for (int j = 0; j < VE; ++j) {
-                        const long long c = (long long)(i * TPR + t) * VE + j;
-                        if (c < a.cols) {
-                            fold[c] = dw[i * VE + j] + (k ? fold[c] : 0.0f);
-                            fold[a.cols + c] = db[i * VE + j] + (k ? fold[a.cols + c] : 0.0f);
-                        }
-                    }
-            }
-            __syncthreads();
-        }
-        for (long long c = threadIdx.x; c < 2 * a.cols; c += kThreads) out[c] = fold[c];
-    } else {
+    float* fold = reinterpret_cast<float*>(smem);
+    for (int k = 0; k < G; ++k) {
+        __syncthreads();
+        if (g != k) continue;
+        float* to = k + 1 == G ? out : fold;
 #pragma unroll
         for (int i = 0; i < NV; ++i)
 #pragma unroll
             for (int j = 0; j < VE; ++j) {
-                const long long c = (long long)(i * TPR + t) * VE + j;
-                if (c < a.cols) { out[c] = dw[i * VE + j]; out[a.cols + c] = db[i * VE + j]; }
+                const int c = (i * TPR + t) * VE + j;
+                if (c < cols) {
+                    to[c] = dw[i * VE + j] + (k ? fold[c] : 0.0f);
+                    to[cols + c] = db[i * VE + j] + (k ? fold[cols + c] : 0.0f);
+                }
             }
     }
 }
@@ -339,6 +576,7 @@ __global__ void __launch_bounds__(32 * kFoldWarps) norm_fold_kernel(const float*
     cudaGridDependencySynchronize();
     float v = 0.0f;
     if (c < 2 * cols)
+#pragma unroll 8
         for (int k = warp; k < n; k += kFoldWarps) v += partials[(long long)k * 2 * cols + c];
     s[warp][lane] = v;
     __syncthreads();
@@ -352,58 +590,83 @@ __global__ void __launch_bounds__(32 * kFoldWarps) norm_fold_kernel(const float*
     else static_cast<__nv_bfloat16*>(out)[at] = __float2bfloat16_rn(v);
 }
 
-// CTAs that fill the device with this kernel, asked once per device and kernel
-struct PerDeviceFill {
-    std::atomic<int> per_sm[64];
-    template <class K> int ctas(K kernel, int threads, size_t smem, int sms) {
-        int dev = 0;
-        if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); return sms; }
-        int n = per_sm[dev & 63].load(std::memory_order_relaxed);
-        if (n == 0) {
-            if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, threads, smem) != cudaSuccess || n < 1) { cudaGetLastError(); n = 1; }
-            per_sm[dev & 63].store(n, std::memory_order_relaxed);
-        }
-        return n * sms;
-    }
-};
+constexpr size_t kRingSmem = 208 * 1024;       // of a block's 227 KB
+
+// Groups and stages of a block for rows of `row_bytes` in `streams` matrices: as many groups as there are threads, but not so many that
+// fewer than two rows fit each one's ring, nor more than give every SM its share of the rows.
+RingPlan ring_plan(const Stream* in, int streams, uint32_t row_bytes, long long rows, int threads, int tpr, int sms) {
+    RingPlan p = {};
+    for (int k = 0; k < streams; ++k) p.in[k] = in[k];
+    p.streams = streams;
+    p.row_bytes = row_bytes;
+    p.stage_bytes = (row_bytes + 15 + 16) / 16 * 16;
+    const size_t row = (size_t)p.stage_bytes * streams;
+    long long g = std::min<long long>({threads / tpr, kMaxGroups, (long long)(kRingSmem / (2 * row)), (rows + sms - 1) / sms});
+    p.groups = (int)std::max<long long>(1, g);
+    p.stages = (int)std::max<size_t>(1, std::min<size_t>(kMaxStages, kRingSmem / (row * p.groups)));
+    return p;
+}
+Stream stream_of(const void* base, long long ld, long long rows, long long cols, int elem) {
+    const char* b = static_cast<const char*>(base);
+    return {b, b + ((rows - 1) * ld + cols) * elem, ld * elem};
+}
 
 template <int DT, int VB, int TPR, int E> cudaError_t forward(const NormArgs& a, int sms, cudaStream_t stream) {
-    constexpr int kThreads = TPR <= 32 ? 128 : TPR, kGroups = kThreads / TPR;
-    static PerDeviceFill fill;
-    const long long want = (a.rows + kGroups - 1) / kGroups;
-    const int cap = fill.ctas(norm_forward_kernel<DT, VB, TPR, E>, kThreads, 0, sms);
-    norm_forward_kernel<DT, VB, TPR, E><<<(unsigned)std::min<long long>(want, cap), kThreads, 0, stream>>>(a);
+    constexpr int kThreads = kForwardThreads<TPR>, kGroups = kThreads / TPR;
+    const long long want = (a.rows + kGroups - 1) / kGroups, cap = (long long)kForwardBlocks<TPR, E> * sms;
+    norm_forward_kernel<DT, VB, TPR, E><<<(unsigned)std::min(want, cap), kThreads, 0, stream>>>(a);
     return cudaGetLastError();
 }
 
-template <int DT, int VB, int TPR, int E> cudaError_t backward(const NormBackArgs& a, int slots, int sms, int* used, cudaStream_t stream) {
-    constexpr int kThreads = TPR <= 32 ? 128 : TPR, kGroups = kThreads / TPR;
-    static PerDeviceFill fill;
-    const size_t smem = kGroups > 1 && a.partials ? 2 * sizeof(float) * (size_t)a.cols : 0;      // at most 8 KB: these rows have 1024 columns or fewer
-    const long long want = (a.rows + kGroups - 1) / kGroups;
-    const int cap = std::min(fill.ctas(norm_backward_kernel<DT, VB, TPR, E>, kThreads, kGroups > 1 ? (size_t)TPR * E * 8 : 0, sms), slots);
-    *used = (int)std::min<long long>(want, cap);
+template <int DT, int VB, int TPR, int E> cudaError_t backward(const NormBackArgs& a, int sms, int* used, cudaStream_t stream) {
+    constexpr int kThreads = kBackwardThreads<TPR, E>, kGroups = kThreads / TPR;
+    const long long want = (a.rows + kGroups - 1) / kGroups, cap = std::min<long long>((long long)kBackwardBlocks<TPR, E> * sms, norm_partial_rows(a.rows, a.cols));
+    *used = (int)std::min(want, cap);
+    const size_t smem = kGroups > 1 && a.partials ? 2 * sizeof(float) * (size_t)a.cols : 0;      // at most 16 KB: these rows have 2048 columns or fewer
     norm_backward_kernel<DT, VB, TPR, E><<<(unsigned)*used, kThreads, smem, stream>>>(a);
     return cudaGetLastError();
 }
 
-// the form for a row of `cols` elements: threads that share it, elements of each
+template <int DT, int VB, int TPR, int E> cudaError_t ring_backward(const NormBackArgs& a, int sms, int* used, cudaStream_t stream) {
+    constexpr int kBytes = RowType<DT>::kBytes;
+    auto kernel = ring_norm_backward_kernel<DT, VB, TPR, E>;
+    static PerDeviceOnce once;
+    const cudaError_t e = once.run([&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRingSmem); });
+    if (e != cudaSuccess) return e;
+    const Stream in[3] = {stream_of(a.dy, a.ld_dy, a.rows, a.cols, kBytes), stream_of(a.h, a.ld_h, a.rows, a.cols, kBytes),
+                          stream_of(a.dsum, a.ld_dsum, a.rows, a.cols, kBytes)};
+    const RingPlan p = ring_plan(in, a.dsum ? 3 : 2, (uint32_t)(a.cols * kBytes), a.rows, 512, TPR, sms);
+    const long long want = (a.rows + p.groups - 1) / p.groups;
+    *used = (int)std::min<long long>({want, (long long)sms, (long long)norm_partial_rows(a.rows, a.cols)});
+    const size_t ring = (size_t)p.groups * p.stages * p.streams * p.stage_bytes, fold = p.groups > 1 ? 2 * sizeof(float) * (size_t)a.cols : 0;
+    kernel<<<(unsigned)*used, p.groups * TPR, std::max(ring, fold), stream>>>(a, p);
+    return cudaGetLastError();
+}
+
+// The form for a row of `cols` elements: threads that share it, elements of each; the fewest threads that keep it in registers, unless
+// measured otherwise (us, the form taken and the other): forward 16384 x 1024 bf16 (128, 8) 29.6, (64, 16) 32.4; over 8192 columns
+// bf16 2000 x 16384 (512, 32) 49.1, (1024, 16) 52.2, fp32 3000 x 9000 (1024, 16) 64.5, (512, 32) 73.2; backward 32768 x 512 bf16
+// (64, 8) 30.1, (128, 8) 46.4; 8000 x 4096 bf16 (256, 16) 53, (512, 8) 68; 2047 x 8191 bf16 in accesses of one (1024, 8) 63.0,
+// (512, 16) 70.1.
 template <int DT, int VB> cudaError_t forward_by_width(const NormArgs& a, int sms, cudaStream_t stream) {
     if (a.cols <= 64) return forward<DT, VB, 8, 8>(a, sms, stream);
     if (a.cols <= 256) return forward<DT, VB, 32, 8>(a, sms, stream);
-    if (a.cols <= 1024) return forward<DT, VB, 32, 32>(a, sms, stream);
-    if (a.cols <= 2048) return forward<DT, VB, 128, 16>(a, sms, stream);
+    if (a.cols <= 512) return forward<DT, VB, 32, 16>(a, sms, stream);
+    if (a.cols <= 1024) return forward<DT, VB, 128, 8>(a, sms, stream);
+    if (a.cols <= 2048) return forward<DT, VB, 256, 8>(a, sms, stream);
     if (a.cols <= 4096) return forward<DT, VB, 256, 16>(a, sms, stream);
     if (a.cols <= 8192) return forward<DT, VB, 512, 16>(a, sms, stream);
-    return forward<DT, VB, 1024, 16>(a, sms, stream);
+    return forward<DT, VB, DT == kBF16 ? 512 : 1024, DT == kBF16 ? 32 : 16>(a, sms, stream);
 }
-template <int DT, int VB> cudaError_t backward_by_width(const NormBackArgs& a, int slots, int sms, int* used, cudaStream_t stream) {
-    if (a.cols <= 64) return backward<DT, VB, 8, 8>(a, slots, sms, used, stream);
-    if (a.cols <= 256) return backward<DT, VB, 32, 8>(a, slots, sms, used, stream);
-    if (a.cols <= 1024) return backward<DT, VB, 32, 32>(a, slots, sms, used, stream);
-    if (a.cols <= 2048) return backward<DT, VB, 128, 16>(a, slots, sms, used, stream);
-    if (a.cols <= 4096) return backward<DT, VB, 256, 16>(a, slots, sms, used, stream);
-    return backward<DT, VB, 512, 16>(a, slots, sms, used, stream);
+template <int DT, int VB> cudaError_t backward_by_width(const NormBackArgs& a, int sms, int* used, cudaStream_t stream) {
+    if (a.cols <= 64) return backward<DT, VB, 8, 8>(a, sms, used, stream);
+    if (a.cols <= 256) return backward<DT, VB, 32, 8>(a, sms, used, stream);
+    if (a.cols <= 512) return backward<DT, VB, 64, 8>(a, sms, used, stream);
+    if (a.cols <= 1024) return backward<DT, VB, 128, 8>(a, sms, used, stream);
+    if (a.cols <= 2048) return backward<DT, VB, 256, 8>(a, sms, used, stream);
+    if (a.cols <= 4096) return backward<DT, VB, 256, 16>(a, sms, used, stream);
+    if (a.cols <= 8192) return backward<DT, VB, VB == 16 ? 512 : 1024, VB == 16 ? 16 : 8>(a, sms, used, stream);
+    return ring_backward<DT, VB, 512, 32>(a, sms, used, stream);
 }
 
 bool aligned(const void* p, long long ld, int elem, int bytes) {
@@ -412,19 +675,13 @@ bool aligned(const void* p, long long ld, int elem, int bytes) {
 
 }  // namespace
 
-constexpr long long kForwardWidth = 16384, kBackwardWidth = 8192;
-
-int norm_partial_rows(long long rows, long long cols) {
-    const long long cap = cols <= 2048 ? 1184 : (cols <= 65536 ? 296 : 64);
-    return (int)std::max<long long>(1, std::min(rows, cap));
-}
 
 cudaError_t launch_norm_forward(NormArgs a, int dtype, int sms, cudaStream_t stream) {
     if (a.rows == 0 || a.cols == 0) return cudaSuccess;
     const int e = dtype == kF32 ? 4 : 2;
     a.weight_vec = (uintptr_t)a.weight % 16 == 0;
     a.bias_vec = (uintptr_t)a.bias % 16 == 0;
-    if (a.cols > kForwardWidth) {
+    if (a.cols > kRingWidth) {
         const unsigned grid = (unsigned)std::min<long long>(a.rows, 2ll * sms);
         if (dtype == kF32) wide_norm_forward_kernel<kF32><<<grid, 1024, 0, stream>>>(a);
         else wide_norm_forward_kernel<kBF16><<<grid, 1024, 0, stream>>>(a);
@@ -435,8 +692,7 @@ cudaError_t launch_norm_forward(NormArgs a, int dtype, int sms, cudaStream_t str
                aligned(a.sum, a.ld_sum, e, bytes) && aligned(a.y, a.ld_y, e, bytes);
     };
     if (dtype == kF32) return all(16) ? forward_by_width<kF32, 16>(a, sms, stream) : forward_by_width<kF32, 4>(a, sms, stream);
-    if (all(16)) return forward_by_width<kBF16, 16>(a, sms, stream);
-    return all(4) ? forward_by_width<kBF16, 4>(a, sms, stream) : forward_by_width<kBF16, 2>(a, sms, stream);
+    return all(16) ? forward_by_width<kBF16, 16>(a, sms, stream) : forward_by_width<kBF16, 2>(a, sms, stream);
 }
 
 cudaError_t launch_norm_backward(NormBackArgs a, int dtype, void* dweight, void* dbias, int sms, cudaStream_t stream) {
@@ -444,12 +700,11 @@ cudaError_t launch_norm_backward(NormBackArgs a, int dtype, void* dweight, void*
     if (!dweight && !dbias) a.partials = nullptr;
     const int e = dtype == kF32 ? 4 : 2;
     a.weight_vec = (uintptr_t)a.weight % 16 == 0;
-    const int slots = norm_partial_rows(a.rows, a.cols);
     int used = 0;
     cudaError_t err = cudaSuccess;
-    if (a.rows > 0 && a.cols > kBackwardWidth) {
+    if (a.rows > 0 && a.cols > kRingWidth) {
         if (a.partials) {
-            used = slots;
+            used = norm_partial_rows(a.rows, a.cols);
             const dim3 grid((unsigned)((a.cols + 127) / 128), (unsigned)used);
             if (dtype == kF32) wide_norm_columns_kernel<kF32><<<grid, 128, 0, stream>>>(a);
             else wide_norm_columns_kernel<kBF16><<<grid, 128, 0, stream>>>(a);
@@ -464,9 +719,8 @@ cudaError_t launch_norm_backward(NormBackArgs a, int dtype, void* dweight, void*
             return (a.cols * e) % bytes == 0 && aligned(a.dy, a.ld_dy, e, bytes) && aligned(a.h, a.ld_h, e, bytes) &&
                    aligned(a.dsum, a.ld_dsum, e, bytes) && aligned(a.dx, a.ld_dx, e, bytes);
         };
-        if (dtype == kF32) err = all(16) ? backward_by_width<kF32, 16>(a, slots, sms, &used, stream) : backward_by_width<kF32, 4>(a, slots, sms, &used, stream);
-        else if (all(16)) err = backward_by_width<kBF16, 16>(a, slots, sms, &used, stream);
-        else err = all(4) ? backward_by_width<kBF16, 4>(a, slots, sms, &used, stream) : backward_by_width<kBF16, 2>(a, slots, sms, &used, stream);
+        if (dtype == kF32) err = all(16) ? backward_by_width<kF32, 16>(a, sms, &used, stream) : backward_by_width<kF32, 4>(a, sms, &used, stream);
+        else err = all(16) ? backward_by_width<kBF16, 16>(a, sms, &used, stream) : backward_by_width<kBF16, 2>(a, sms, &used, stream);
     }
     if (err != cudaSuccess || (!dweight && !dbias)) return err;
     // rows == 0: nothing was launched and the sums over no rows are zeros (used == 0)

@@ -159,16 +159,33 @@ template <int WIDTH> __device__ __forceinline__ float group_max(float v) {
     }
 }
 
-// Sum over the TPR threads of a row (a power of two; the CTA holds one row where TPR > 32).  `buf` holds TPR / 32 floats, and
-// two calls in a row use different ones: the barrier of the second keeps the first one's readers apart from its next writer.
+// Sums over the TPR threads of a row (a power of two); a block holds blockDim / TPR rows side by side, each with a named barrier of its
+// own where TPR > 32.  `buf` holds blockDim / 32 entries, and two calls in a row use different ones: the barrier of the second
+// keeps the first one's readers apart from its next writer.
+template <int TPR> __device__ __forceinline__ void row_barrier() {
+    if constexpr (TPR <= 32) __syncwarp();
+    else asm volatile("bar.sync %0, %1;" ::"r"(1 + (int)threadIdx.x / TPR), "n"(TPR) : "memory");
+}
 template <int TPR> __device__ __forceinline__ float row_sum(float v, float* buf) {
     if constexpr (TPR <= 32) return group_sum<TPR>(v);
     else {
+        constexpr int W = TPR / 32;
         v = group_sum<32>(v);
         if ((threadIdx.x & 31) == 0) buf[threadIdx.x >> 5] = v;
-        __syncthreads();
-        const float t = (threadIdx.x & 31) < TPR / 32 ? buf[threadIdx.x & 31] : 0.0f;
-        return group_sum<32>(t);
+        row_barrier<TPR>();
+        const float t = buf[(threadIdx.x / TPR) * W + (threadIdx.x & (W - 1))];
+        return group_sum<W>(t);
+    }
+}
+template <int TPR> __device__ __forceinline__ float2 row_sum2(float2 v, float2* buf) {
+    if constexpr (TPR <= 32) return make_float2(group_sum<TPR>(v.x), group_sum<TPR>(v.y));
+    else {
+        constexpr int W = TPR / 32;
+        v = make_float2(group_sum<32>(v.x), group_sum<32>(v.y));
+        if ((threadIdx.x & 31) == 0) buf[threadIdx.x >> 5] = v;
+        row_barrier<TPR>();
+        const float2 t = buf[(threadIdx.x / TPR) * W + (threadIdx.x & (W - 1))];
+        return make_float2(group_sum<W>(t.x), group_sum<W>(t.y));
     }
 }
 
