@@ -11,7 +11,7 @@
 // reductions and the output: it is read once.  Groups go through the rows with a stride and ask for the next row before they
 // reduce this one; several groups an SM cover each other's latency.
 // Measured, copy bandwidth 6.55 TB/s: forward with residual and sum 16384 x 1024 bf16 29.6 us (4.5 TB/s), 8000 x 4096 bf16 27.6 us
-// (4.8), 4097 x 1001 fp32 11.9 us; backward 16384 x 1024 bf16 with dsum 32.7 us (4.1), fp32 38.7 us (5.2), 2047 x 8191 bf16 63 us.
+// (4.8), 4097 x 1001 fp32 11.9 us; backward 16384 x 1024 bf16 with dsum 32.7 us (4.1), fp32 36.3 us (5.6), 2047 x 8191 bf16 57.0 us.
 // The centred squares are summed after the mean is known (no difference of large numbers); the normalised value uses the sum
 // before it is rounded for sum_out: one rounding, at the end.
 // A thread owns the same columns of every row, so the backward pass keeps its share of dw and db in registers over all rows
@@ -218,6 +218,14 @@ template <int DT, int VB, int TPR, int E> struct RowRegs {
             else f[i] = to_float(u[i]);
         }
     }
+    // brings row r of two matrices to L2, a line a thread: half the threads cover a row of E <= 16
+    static __device__ __forceinline__ void fetch(const void* a, long long ld_a, const void* b, long long ld_b, long long r, long long rows, int cols) {
+        const int t = threadIdx.x % TPR, c = (t & (TPR / 2 - 1)) * (128 / (int)sizeof(T));
+        if (r < rows && c < cols) {
+            const T* p = t < TPR / 2 ? row_of<DT>(a, ld_a, r) + c : row_of<DT>(b, ld_b, r) + c;
+            asm volatile("prefetch.global.L2 [%0];" ::"l"(p));
+        }
+    }
     static __device__ __forceinline__ void store(T* row, int cols, const float2 (&v)[E / 2]) {
         const float* f = reinterpret_cast<const float*>(v);
 #pragma unroll
@@ -245,7 +253,8 @@ __global__ void __launch_bounds__(kForwardThreads<TPR>, kForwardBlocks<TPR, E>) 
     // kAhead: the next row is asked for before this one is reduced, where the registers suffice.  Without and with, us: 16384 x 1024
     // bf16 50.2 and 29.6, 32768 x 512 bf16 21.5 and 15.4, 8000 x 4096 bf16 35.7 and 27.6, 2047 x 8191 bf16 41.9 and 26.3; where they
     // do not (8 elements in accesses of one, fp32) 4097 x 1001 13.9 and 15.7.  kKeep: weight and bias stay in registers over all rows.
-    constexpr bool kAhead = VB == 16 ? DT == kBF16 || R::NV <= 2 : E == 16 && (TPR == 256 || TPR == 512), kKeep = E < 32;
+    // kFetch: otherwise the next row is brought to L2; 2048 x 8192 fp32 38.4 without and 30.0 with, 3000 x 9000 fp32 64.9 and 49.2.
+    constexpr bool kAhead = VB == 16 ? DT == kBF16 || R::NV <= 2 : E == 16 && (TPR == 256 || TPR == 512), kKeep = E < 32, kFetch = !kAhead && TPR >= 128;
     __shared__ float buf[2][32];
     const int t = threadIdx.x % TPR, g = threadIdx.x / TPR, cols = (int)a.cols;
     const float inv_n = 1.0f / (float)a.cols;
@@ -278,6 +287,7 @@ __global__ void __launch_bounds__(kForwardThreads<TPR>, kForwardBlocks<TPR, E>) 
             for (int k = 0; k < P; ++k) h[k] = __fadd2_rn(h[k], s[k]);
         }
         ask(r + step);
+        if constexpr (kFetch) R::fetch(a.x, a.ld_x, a.residual ? a.residual : a.x, a.residual ? a.ld_residual : a.ld_x, r + step, a.rows, cols);
         if (a.sum && on) R::store(row_of<DT>(a.sum, a.ld_sum, r), cols, h);
         float2 add = h[0];
 #pragma unroll
@@ -341,8 +351,9 @@ __global__ void __launch_bounds__(kBackwardThreads<TPR, E>, kBackwardBlocks<TPR,
     using R = RowRegs<DT, VB, TPR, E>;
     constexpr int P = E / 2, kThreads = kBackwardThreads<TPR, E>, kGroups = kThreads / TPR;
     // As in the forward kernel.  Without and with asking ahead, us: 16384 x 1024 bf16 38.3 and 32.7; fp32 spills: 30000 x 100 20.1
-    // and 26.2.
-    constexpr bool kAhead = VB == 16 && DT == kBF16, kKeep = TPR < 1024;
+    // and 26.2.  kFetch without and with: 2048 x 8192 fp32 58.0 and 43.5, 2047 x 8191 bf16 63.6 and 57.0; but 4097 x 1001 fp32, in accesses
+    // of one and 128 threads a row, 15.8 and 18.3.
+    constexpr bool kAhead = VB == 16 && DT == kBF16, kKeep = TPR < 1024, kFetch = !kAhead && (TPR == 1024 || (VB == 16 && TPR >= 128));
     __shared__ float2 buf[2][32];
     extern __shared__ float fold[];                       // kGroups > 1: [2][cols]
     const int g = threadIdx.x / TPR, cols = (int)a.cols;
@@ -383,6 +394,10 @@ __global__ void __launch_bounds__(kBackwardThreads<TPR, E>, kBackwardBlocks<TPR,
             mean = on ? a.mean[r] : 0.0f;
             rstd = on ? a.rstd[r] : 0.0f;
             R::load(row_of<DT>(a.dsum, a.ld_dsum, r), on && a.dsum ? cols : 0, e);
+        }
+        if constexpr (kFetch) {
+            R::fetch(a.dy, a.ld_dy, a.h, a.ld_h, r + step, a.rows, cols);
+            if constexpr (VB == 16) if (a.dsum) R::fetch(a.dsum, a.ld_dsum, a.dsum, a.ld_dsum, r + step, a.rows, cols);
         }
         ask(r + step);
         const float2 minus = make_float2(-mean, -mean), rs = make_float2(rstd, rstd);
@@ -645,9 +660,10 @@ template <int DT, int VB, int TPR, int E> cudaError_t ring_backward(const NormBa
 
 // The form for a row of `cols` elements: threads that share it, elements of each; the fewest threads that keep it in registers, unless
 // measured otherwise (us, the form taken and the other): forward 16384 x 1024 bf16 (128, 8) 29.6, (64, 16) 32.4; over 8192 columns
-// bf16 2000 x 16384 (512, 32) 49.1, (1024, 16) 52.2, fp32 3000 x 9000 (1024, 16) 64.5, (512, 32) 73.2; backward 32768 x 512 bf16
+// bf16 2000 x 16384 (512, 32) 49.1, (1024, 16) 52.2, fp32 3000 x 9000 (1024, 16) 64.5, (512, 32) 73.2 (both without kFetch); backward 32768 x 512 bf16
 // (64, 8) 30.1, (128, 8) 46.4; 8000 x 4096 bf16 (256, 16) 53, (512, 8) 68; 2047 x 8191 bf16 in accesses of one (1024, 8) 63.0,
-// (512, 16) 70.1.
+// (512, 16) 70.1 (both without kFetch).  Accesses of 16 bytes around such a row's elements, shifted into place, were no faster there
+// (61.2) and slower forward (38.0 against 25.7).
 template <int DT, int VB> cudaError_t forward_by_width(const NormArgs& a, int sms, cudaStream_t stream) {
     if (a.cols <= 64) return forward<DT, VB, 8, 8>(a, sms, stream);
     if (a.cols <= 256) return forward<DT, VB, 32, 8>(a, sms, stream);
