@@ -292,14 +292,14 @@ __global__ void __launch_bounds__(kForwardThreads<TPR>, kForwardBlocks<TPR, E>) 
         float2 add = h[0];
 #pragma unroll
         for (int k = 1; k < P; ++k) add = __fadd2_rn(add, h[k]);
-        const float mean = row_sum<TPR>(add.x + add.y, buf[0]) * inv_n;
+        const float mean = row_sum<TPR, kGroups>(add.x + add.y, buf[0]) * inv_n;
         float2 sq = make_float2(0.0f, 0.0f);
 #pragma unroll
         for (int k = 0; k < P; ++k) {
             h[k] = __fadd2_rn(h[k], R::inside(k, cols, -mean));      // the zeros past the last column stay zeros
             sq = __ffma2_rn(h[k], h[k], sq);
         }
-        const float rstd = rsqrtf(row_sum<TPR>(sq.x + sq.y, buf[1]) * inv_n + a.eps);
+        const float rstd = rsqrtf(row_sum<TPR, kGroups>(sq.x + sq.y, buf[1]) * inv_n + a.eps);
         if (!on) continue;
         if (t == 0) {
             if (a.mean) a.mean[r] = mean;
@@ -412,7 +412,7 @@ __global__ void __launch_bounds__(kBackwardThreads<TPR, E>, kBackwardBlocks<TPR,
             s1 = __fadd2_rn(s1, d[k]);
             s2 = __ffma2_rn(d[k], x[k], s2);
         }
-        const float2 both = row_sum2<TPR>(make_float2(s1.x + s1.y, s2.x + s2.y), buf[turn]);
+        const float2 both = row_sum2<TPR, kGroups>(make_float2(s1.x + s1.y, s2.x + s2.y), buf[turn]);
         if (!on) continue;
         const float m1 = -both.x * inv_n, m2 = -both.y * inv_n;
         const float2 mm1 = make_float2(m1, m1), mm2 = make_float2(m2, m2);

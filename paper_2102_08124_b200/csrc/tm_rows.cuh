@@ -159,31 +159,32 @@ template <int WIDTH> __device__ __forceinline__ float group_max(float v) {
     }
 }
 
-// Sums over the TPR threads of a row (a power of two); a block holds blockDim / TPR rows side by side, each with a named barrier of its
-// own where TPR > 32.  `buf` holds blockDim / 32 entries, and two calls in a row use different ones: the barrier of the second
+// Sums over the TPR threads of a row (a power of two); a block holds GROUPS = blockDim / TPR rows side by side, each with a named barrier
+// of its own where TPR > 32 and GROUPS > 1 (a block that names barriers at run time takes all 16 of them, of the 64 of an SM).  `buf` holds blockDim / 32 entries, and two calls in a row use different ones: the barrier of the second
 // keeps the first one's readers apart from its next writer.
-template <int TPR> __device__ __forceinline__ void row_barrier() {
+template <int TPR, int GROUPS = 1> __device__ __forceinline__ void row_barrier() {
     if constexpr (TPR <= 32) __syncwarp();
+    else if constexpr (GROUPS == 1) __syncthreads();
     else asm volatile("bar.sync %0, %1;" ::"r"(1 + (int)threadIdx.x / TPR), "n"(TPR) : "memory");
 }
-template <int TPR> __device__ __forceinline__ float row_sum(float v, float* buf) {
+template <int TPR, int GROUPS = 1> __device__ __forceinline__ float row_sum(float v, float* buf) {
     if constexpr (TPR <= 32) return group_sum<TPR>(v);
     else {
         constexpr int W = TPR / 32;
         v = group_sum<32>(v);
         if ((threadIdx.x & 31) == 0) buf[threadIdx.x >> 5] = v;
-        row_barrier<TPR>();
+        row_barrier<TPR, GROUPS>();
         const float t = buf[(threadIdx.x / TPR) * W + (threadIdx.x & (W - 1))];
         return group_sum<W>(t);
     }
 }
-template <int TPR> __device__ __forceinline__ float2 row_sum2(float2 v, float2* buf) {
+template <int TPR, int GROUPS = 1> __device__ __forceinline__ float2 row_sum2(float2 v, float2* buf) {
     if constexpr (TPR <= 32) return make_float2(group_sum<TPR>(v.x), group_sum<TPR>(v.y));
     else {
         constexpr int W = TPR / 32;
         v = make_float2(group_sum<32>(v.x), group_sum<32>(v.y));
         if ((threadIdx.x & 31) == 0) buf[threadIdx.x >> 5] = v;
-        row_barrier<TPR>();
+        row_barrier<TPR, GROUPS>();
         const float2 t = buf[(threadIdx.x / TPR) * W + (threadIdx.x & (W - 1))];
         return make_float2(group_sum<W>(t.x), group_sum<W>(t.y));
     }
