@@ -10,8 +10,8 @@
 // A row belongs to a group of threads -- 8 or 32 of a warp, or up to 1024, by its width -- and stays in their registers between the
 // reductions and the output: it is read once.  Groups go through the rows with a stride and ask for the next row before they
 // reduce this one; several groups an SM cover each other's latency.
-// Measured, copy bandwidth 6.55 TB/s: forward with residual and sum 16384 x 1024 bf16 29.6 us (4.5 TB/s), 8000 x 4096 bf16 27.6 us
-// (4.8), 4097 x 1001 fp32 11.9 us; backward 16384 x 1024 bf16 with dsum 32.7 us (4.1), fp32 36.3 us (5.6), 2047 x 8191 bf16 57.0 us.
+// Measured, copy bandwidth 6.55 TB/s: forward with residual and sum 16384 x 1024 bf16 23.1 us (5.8 TB/s), 8000 x 4096 bf16 27.1 us
+// (4.8), 4097 x 1001 fp32 7.8 us (4.2); backward 16384 x 1024 bf16 with dsum 33.1 us (4.1), fp32 36.3 us (5.6), 2047 x 8191 bf16 57.0 us.
 // The centred squares are summed after the mean is known (no difference of large numbers); the normalised value uses the sum
 // before it is rounded for sum_out: one rounding, at the end.
 // A thread owns the same columns of every row, so the backward pass keeps its share of dw and db in registers over all rows
@@ -250,10 +250,9 @@ template <int DT, int VB, int TPR, int E>
 __global__ void __launch_bounds__(kForwardThreads<TPR>, kForwardBlocks<TPR, E>) norm_forward_kernel(const NormArgs a) {
     using R = RowRegs<DT, VB, TPR, E>;
     constexpr int P = E / 2, kGroups = kForwardThreads<TPR> / TPR;
-    // kAhead: the next row is asked for before this one is reduced, where the registers suffice.  Without and with, us: 16384 x 1024
-    // bf16 50.2 and 29.6, 32768 x 512 bf16 21.5 and 15.4, 8000 x 4096 bf16 35.7 and 27.6, 2047 x 8191 bf16 41.9 and 26.3; where they
-    // do not (8 elements in accesses of one, fp32) 4097 x 1001 13.9 and 15.7.  kKeep: weight and bias stay in registers over all rows.
-    // kFetch: otherwise the next row is brought to L2; 2048 x 8192 fp32 38.4 without and 30.0 with, 3000 x 9000 fp32 64.9 and 49.2.
+    // kAhead: the next row is asked for before this one is reduced, where the registers suffice; kFetch: else it is brought to L2.  Neither
+    // and as here, us: 16384 x 1024 bf16 31.3 and 23.1, 8000 x 4096 bf16 34.9 and 27.1, 2047 x 8191 bf16 41.5 and 26.1, 2048 x 8192 fp32
+    // 37.7 and 29.6, 3000 x 9000 fp32 64.4 and 49.2; 200 x 12000 bf16 8.6 and 9.2.  kKeep: weight and bias stay in registers over all rows.
     constexpr bool kAhead = VB == 16 ? DT == kBF16 || R::NV <= 2 : E == 16 && (TPR == 256 || TPR == 512), kKeep = E < 32, kFetch = !kAhead && TPR >= 128;
     __shared__ float buf[2][32];
     const int t = threadIdx.x % TPR, g = threadIdx.x / TPR, cols = (int)a.cols;
@@ -659,19 +658,22 @@ template <int DT, int VB, int TPR, int E> cudaError_t ring_backward(const NormBa
 }
 
 // The form for a row of `cols` elements: threads that share it, elements of each; the fewest threads that keep it in registers, unless
-// measured otherwise (us, the form taken and the other): forward 16384 x 1024 bf16 (128, 8) 29.6, (64, 16) 32.4; over 8192 columns
-// bf16 2000 x 16384 (512, 32) 49.1, (1024, 16) 52.2, fp32 3000 x 9000 (1024, 16) 64.5, (512, 32) 73.2 (both without kFetch); backward 32768 x 512 bf16
-// (64, 8) 30.1, (128, 8) 46.4; 8000 x 4096 bf16 (256, 16) 53, (512, 8) 68; 2047 x 8191 bf16 in accesses of one (1024, 8) 63.0,
+// measured otherwise (us, the form taken and the other): forward 16384 x 1024 bf16 (128, 8) 23.1, (64, 16) 24.3; 4097 x 1001 fp32 (64, 16)
+// 7.8, (128, 8) 9.1; 16384 x 2048 bf16 (128, 16) 27.8, (256, 8) 29.6; 2048 x 8192 fp32 (1024, 8) 25.6, (512, 16) 29.6; 2047 x 8191 bf16
+// (512, 16) 26.1, (1024, 8) 39.0; wider bf16 (512, 32) 2000 x 16384 51.5 and 200 x 12000 9.2, (1024, 16) 45.2 and 11.3; 3000 x 9000 fp32
+// (1024, 16) 49.2, (512, 32) 66.0; backward 32768 x 512 bf16
+// (64, 8) 30.1, (128, 8) 46.4; 8000 x 4096 bf16 (256, 16) 53.2, (512, 8) 68.4; 2047 x 8191 bf16 in accesses of one (1024, 8) 63.0,
 // (512, 16) 70.1 (both without kFetch).  Accesses of 16 bytes around such a row's elements, shifted into place, were no faster there
 // (61.2) and slower forward (38.0 against 25.7).
 template <int DT, int VB> cudaError_t forward_by_width(const NormArgs& a, int sms, cudaStream_t stream) {
     if (a.cols <= 64) return forward<DT, VB, 8, 8>(a, sms, stream);
     if (a.cols <= 256) return forward<DT, VB, 32, 8>(a, sms, stream);
     if (a.cols <= 512) return forward<DT, VB, 32, 16>(a, sms, stream);
-    if (a.cols <= 1024) return forward<DT, VB, 128, 8>(a, sms, stream);
-    if (a.cols <= 2048) return forward<DT, VB, 256, 8>(a, sms, stream);
+    if (a.cols <= 1024) return forward<DT, VB, VB == 16 ? 128 : 64, VB == 16 ? 8 : 16>(a, sms, stream);
+    if (a.cols <= 2048) return forward<DT, VB, 128, 16>(a, sms, stream);
     if (a.cols <= 4096) return forward<DT, VB, 256, 16>(a, sms, stream);
-    if (a.cols <= 8192) return forward<DT, VB, 512, 16>(a, sms, stream);
+    constexpr bool kWords = VB == 16 && DT == kF32;
+    if (a.cols <= 8192) return forward<DT, VB, kWords ? 1024 : 512, kWords ? 8 : 16>(a, sms, stream);
     return forward<DT, VB, DT == kBF16 ? 512 : 1024, DT == kBF16 ? 32 : 16>(a, sms, stream);
 }
 template <int DT, int VB> cudaError_t backward_by_width(const NormBackArgs& a, int sms, int* used, cudaStream_t stream) {
