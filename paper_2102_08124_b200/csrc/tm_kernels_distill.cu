@@ -20,7 +20,6 @@ namespace {
 
 constexpr double kLog2eD = 1.4426950408889634074, kLn2D = 0.69314718055994530942;
 
-__device__ __forceinline__ float warp_sum(float v) { return group_sum<32>(v); }
 __device__ __forceinline__ double warp_sum_double(double v) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);

@@ -36,7 +36,7 @@ int norm_partial_rows(long long rows, long long cols) {
 
 namespace {
 
-constexpr int kMaxStages = 4, kMaxGroups = 16, kMaxStreams = 3;
+constexpr int kMaxStages = 4, kMaxStreams = 3;
 
 // The rows of one input matrix as they are copied: [begin, end) is the memory that the matrix covers, first to last element.
 struct Stream {
@@ -58,7 +58,7 @@ struct RowBytes {
     }
 };
 struct RingPlan {
-    int groups, stages, streams;
+    int stages, streams;
     uint32_t row_bytes, stage_bytes;           // of one stream: a row, a stage
     Stream in[kMaxStreams];
 };
@@ -80,8 +80,8 @@ template <int DT, int VB> struct Access {
     }
 };
 
-// A group's ring: rows n = 0, 1, ... of the group go through its stages in turn.
-struct GroupRing {
+// A block's ring: its rows go through the stages in turn.
+struct RowRing {
     const RingPlan& plan;
     char* stage0;
     uint64_t* bars;
@@ -160,17 +160,16 @@ template <int DT> __device__ __forceinline__ typename RowType<DT>::T* row_of(voi
     return static_cast<typename RowType<DT>::T*>(p) + r * ld;
 }
 
-// Sets a block's rings up and starts them; returns this group's.
-template <int TPR> __device__ __forceinline__ GroupRing start_ring(const RingPlan& plan, char* smem, uint64_t* bars, long long first, long long step, long long rows) {
-    const int g = threadIdx.x / TPR, S = plan.stages;
+// Sets a block's ring up and asks for its first rows
+__device__ __forceinline__ RowRing start_ring(const RingPlan& plan, char* smem, uint64_t* bars, long long first, long long step, long long rows) {
+    const RowRing ring{plan, smem, bars};
     if (threadIdx.x == 0) {
-        for (int i = 0; i < plan.groups * S; ++i) mbar_init(bars + i, 1);
+        for (int i = 0; i < plan.stages; ++i) mbar_init(bars + i, 1);
         fence_mbar_init();
     }
     __syncthreads();
-    const GroupRing ring{plan, smem + (size_t)g * S * plan.streams * plan.stage_bytes, bars + g * S};
-    if (threadIdx.x % TPR == 0)
-        for (int k = 0; k < S; ++k) { const long long r = first + k * step; if (r < rows) ring.ask(k, r); }
+    if (threadIdx.x == 0)
+        for (int k = 0; k < plan.stages; ++k) { const long long r = first + k * step; if (r < rows) ring.ask(k, r); }
     return ring;
 }
 
@@ -443,20 +442,21 @@ __global__ void __launch_bounds__(kBackwardThreads<TPR, E>, kBackwardBlocks<TPR,
 }
 
 // Rows of 8193 to kRingWidth columns: two rows' inputs do not fit the registers beside the parameters' gradients, so bulk copies bring the
-// next rows to shared memory.  2000 x 16384 bf16 87 us, 3000 x 9000 fp32 87 us; with every step read from L2 again 198 and 186 us.  For
+// next rows to shared memory.  2000 x 16384 bf16 86 us, 3000 x 9000 fp32 85 us; with every step read from L2 again 198 and 186 us.  For
 // narrower rows the registers are faster: 16384 x 1024 bf16 77 us by this kernel, 32.7 us by the one above.
 // streams: dy, h and, with a third one, dsum
-template <int DT, int VB, int TPR, int E>
-__global__ void __launch_bounds__(512, 1) ring_norm_backward_kernel(const __grid_constant__ NormBackArgs a, const __grid_constant__ RingPlan plan) {
+constexpr int kRingThreads = 512;
+template <int DT, int VB, int E>
+__global__ void __launch_bounds__(kRingThreads, 1) ring_norm_backward_kernel(const __grid_constant__ NormBackArgs a, const __grid_constant__ RingPlan plan) {
     using A = Access<DT, VB>;
-    constexpr int VE = A::kElems, NV = E / VE;
+    constexpr int VE = A::kElems, NV = E / VE, TPR = kRingThreads;
     extern __shared__ __align__(128) char smem[];
-    __shared__ __align__(8) uint64_t bars[kMaxGroups * kMaxStages];
+    __shared__ __align__(8) uint64_t bars[kMaxStages];
     __shared__ float2 buf[2][32];
-    const int t = threadIdx.x % TPR, g = threadIdx.x / TPR, G = plan.groups, cols = (int)a.cols;
+    const int t = threadIdx.x, cols = (int)a.cols;
     const float inv_n = 1.0f / (float)a.cols;
-    const long long first = (long long)blockIdx.x * G + g, step = (long long)gridDim.x * G;
-    const GroupRing ring = start_ring<TPR>(plan, smem, bars, first, step, a.rows);
+    const long long first = blockIdx.x, step = gridDim.x;
+    const RowRing ring = start_ring(plan, smem, bars, first, step, a.rows);
     float dw[E], db[E];
 #pragma unroll
     for (int k = 0; k < E; ++k) dw[k] = db[k] = 0.0f;
@@ -518,24 +518,17 @@ __global__ void __launch_bounds__(512, 1) ring_norm_backward_kernel(const __grid
         if (++slot == plan.stages) { slot = 0; phase ^= 1u; }
     }
     if (!a.partials) return;
-    // the groups add their columns one after the other; the rings are done with
     float* out = a.partials + (long long)blockIdx.x * 2 * a.cols;
-    float* fold = reinterpret_cast<float*>(smem);
-    for (int k = 0; k < G; ++k) {
-        __syncthreads();
-        if (g != k) continue;
-        float* to = k + 1 == G ? out : fold;
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
+    for (int i = 0; i < NV; ++i)
 #pragma unroll
-            for (int j = 0; j < VE; ++j) {
-                const int c = (i * TPR + t) * VE + j;
-                if (c < cols) {
-                    to[c] = dw[i * VE + j] + (k ? fold[c] : 0.0f);
-                    to[cols + c] = db[i * VE + j] + (k ? fold[cols + c] : 0.0f);
-                }
+        for (int j = 0; j < VE; ++j) {
+            const int c = (i * TPR + t) * VE + j;
+            if (c < cols) {
+                out[c] = dw[i * VE + j];
+                out[cols + c] = db[i * VE + j];
             }
-    }
+        }
 }
 
 template <int DT> __global__ void __launch_bounds__(1024) wide_norm_backward_kernel(const NormBackArgs a) {
@@ -606,18 +599,14 @@ __global__ void __launch_bounds__(32 * kFoldWarps) norm_fold_kernel(const float*
 
 constexpr size_t kRingSmem = 208 * 1024;       // of a block's 227 KB
 
-// Groups and stages of a block for rows of `row_bytes` in `streams` matrices: as many groups as there are threads, but not so many that
-// fewer than two rows fit each one's ring, nor more than give every SM its share of the rows.
-RingPlan ring_plan(const Stream* in, int streams, uint32_t row_bytes, long long rows, int threads, int tpr, int sms) {
+// As many stages as fit, for rows of `row_bytes` in `streams` matrices (at least one: 3 x 64 KB)
+RingPlan ring_plan(const Stream* in, int streams, uint32_t row_bytes) {
     RingPlan p = {};
     for (int k = 0; k < streams; ++k) p.in[k] = in[k];
     p.streams = streams;
     p.row_bytes = row_bytes;
     p.stage_bytes = (row_bytes + 15 + 16) / 16 * 16;
-    const size_t row = (size_t)p.stage_bytes * streams;
-    long long g = std::min<long long>({threads / tpr, kMaxGroups, (long long)(kRingSmem / (2 * row)), (rows + sms - 1) / sms});
-    p.groups = (int)std::max<long long>(1, g);
-    p.stages = (int)std::max<size_t>(1, std::min<size_t>(kMaxStages, kRingSmem / (row * p.groups)));
+    p.stages = (int)std::min<size_t>(kMaxStages, kRingSmem / ((size_t)p.stage_bytes * streams));
     return p;
 }
 Stream stream_of(const void* base, long long ld, long long rows, long long cols, int elem) {
@@ -641,19 +630,17 @@ template <int DT, int VB, int TPR, int E> cudaError_t backward(const NormBackArg
     return cudaGetLastError();
 }
 
-template <int DT, int VB, int TPR, int E> cudaError_t ring_backward(const NormBackArgs& a, int sms, int* used, cudaStream_t stream) {
+template <int DT, int VB, int E> cudaError_t ring_backward(const NormBackArgs& a, int sms, int* used, cudaStream_t stream) {
     constexpr int kBytes = RowType<DT>::kBytes;
-    auto kernel = ring_norm_backward_kernel<DT, VB, TPR, E>;
+    auto kernel = ring_norm_backward_kernel<DT, VB, E>;
     static PerDeviceOnce once;
     const cudaError_t e = once.run([&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRingSmem); });
     if (e != cudaSuccess) return e;
     const Stream in[3] = {stream_of(a.dy, a.ld_dy, a.rows, a.cols, kBytes), stream_of(a.h, a.ld_h, a.rows, a.cols, kBytes),
                           stream_of(a.dsum, a.ld_dsum, a.rows, a.cols, kBytes)};
-    const RingPlan p = ring_plan(in, a.dsum ? 3 : 2, (uint32_t)(a.cols * kBytes), a.rows, 512, TPR, sms);
-    const long long want = (a.rows + p.groups - 1) / p.groups;
-    *used = (int)std::min<long long>({want, (long long)sms, (long long)norm_partial_rows(a.rows, a.cols)});
-    const size_t ring = (size_t)p.groups * p.stages * p.streams * p.stage_bytes, fold = p.groups > 1 ? 2 * sizeof(float) * (size_t)a.cols : 0;
-    kernel<<<(unsigned)*used, p.groups * TPR, std::max(ring, fold), stream>>>(a, p);
+    const RingPlan p = ring_plan(in, a.dsum ? 3 : 2, (uint32_t)(a.cols * kBytes));
+    *used = std::min(sms, norm_partial_rows(a.rows, a.cols));
+    kernel<<<(unsigned)*used, kRingThreads, (size_t)p.stages * p.streams * p.stage_bytes, stream>>>(a, p);
     return cudaGetLastError();
 }
 
@@ -684,7 +671,7 @@ template <int DT, int VB> cudaError_t backward_by_width(const NormBackArgs& a, i
     if (a.cols <= 2048) return backward<DT, VB, 256, 8>(a, sms, used, stream);
     if (a.cols <= 4096) return backward<DT, VB, 256, 16>(a, sms, used, stream);
     if (a.cols <= 8192) return backward<DT, VB, VB == 16 ? 512 : 1024, VB == 16 ? 16 : 8>(a, sms, used, stream);
-    return ring_backward<DT, VB, 512, 32>(a, sms, used, stream);
+    return ring_backward<DT, VB, 32>(a, sms, used, stream);
 }
 
 bool aligned(const void* p, long long ld, int elem, int bytes) {
