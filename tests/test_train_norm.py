@@ -113,6 +113,23 @@ def test_outputs_on_inputs_and_without_parameters(cols, dtype):
         assert torch.equal(dx2, dx) and torch.equal(dw2, dw) and torch.equal(db2, db), name
 
 
+@pytest.mark.parametrize("rows,cols,dtype", [(20000, 24, "f32"), (9000, 300, "bf16"), (5000, 1024, "bf16"), (5000, 1001, "f32"), (2500, 4095, "bf16"), (900, 8192, "f32"), (700, 9000, "bf16")])
+def test_outputs_on_inputs_with_many_rows(rows, cols, dtype):
+    """Rows are read ahead of their turn while others are written: the same bits as with outputs of their own."""
+    rng = np.random.Generator(np.random.PCG64(8))
+    x, _ = _matrix(rng, rows, cols, dtype)
+    r, _ = _matrix(rng, rows, cols, dtype)
+    y, s, mean, rstd = tm.tm_layer_norm(x, residual=r)
+    dx, dw, db = tm.tm_layer_norm_backward(x, s, mean, rstd, dsum=r)
+    for name in ("dy", "h", "dsum"):
+        t = {"dy": x.clone(), "h": s.clone(), "dsum": r.clone()}
+        dx2, dw2, db2 = tm.tm_layer_norm_backward(t["dy"], t["h"], mean, rstd, dsum=t["dsum"], dx=t[name])
+        assert torch.equal(dx2, dx) and torch.equal(dw2, dw) and torch.equal(db2, db), name
+    x2, r2 = x.clone(), r.clone()
+    tm.tm_layer_norm(x2, residual=r2, y=r2, sum_out=x2)
+    assert torch.equal(r2, y) and torch.equal(x2, s)
+
+
 def test_degenerate_rows():
     """Constant rows (no variance), rows of one column, no rows, a large offset."""
     for cols in (1, 8, 1000, 4096, 17000):
