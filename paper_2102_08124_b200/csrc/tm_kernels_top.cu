@@ -151,7 +151,8 @@ template <int DT> __device__ __noinline__ void offer_vector(uint4 q, float least
     }
 }
 
-// Collects the entries at or above the bound one vector of each thread at a time, with a look at the buffer after each.  All threads.
+// Collects the entries at or above the bound one vector of each thread at a time, with a look at the buffer after each.  All threads,
+// none of which may still have to read the count when the first one enters.
 template <int DT, int NT> __device__ __noinline__ void collect_slowly(unsigned long long* buf, Work& w, const uint4* vec, int inside, unsigned long long bound, long long column,
                                                                       int have) {
     constexpr int V = RowType<DT>::kVec;
@@ -276,7 +277,9 @@ template <int DT, int NT> __global__ void __launch_bounds__(NT, kBlocks<NT>) top
             }
         });
         __syncthreads();
-        if (work.count > kRoom - 32) collect_slowly<DT, NT>(buf, work, vec, inside, bound, slice.column, have);
+        const bool over = work.count > kRoom - 32;
+        __syncthreads();                                  // everybody has read the count that the next function sets back
+        if (over) collect_slowly<DT, NT>(buf, work, vec, inside, bound, slice.column, have);
         if (tid < edges) {
             const long long c = slice.edge(tid);
             const float v = to_float(row.base[c]), old = m;
