@@ -293,10 +293,13 @@ int tm_layer_norm_backward(const void* dy, int64_t ld_dy, const void* h, int64_t
  *                      p_rest = max(0, 1 - sum_k p_k), one class for all logits that are not listed, q_rest their sum;
  *   loss = f * (sum_k p_k * (log p_k - log q_k) + p_rest * (log p_rest - log q_rest));
  *   dlogits_j = f / temperature * (q_j - p_j) for a listed logit, f / temperature * (q_j - p_rest * q_j / q_rest) for another.
- * Terms with p_k = 0 are left out, and so is that of p_rest where q_rest = 0.  An entry whose id is negative is padding (lists of different
- * lengths); one whose id is not below vocab, or stood in the row before, is left out too and raises TM_DEV_BADID in *status_dev.
+ * Terms with p_k = 0 are left out, and so is that of p_rest where the student has no mass outside the list: unlisted logits of -Inf, or
+ * more than 2^20 binades of exp(logit / temperature) below the listed ones, which only masks are (the type's lowest value, say).  Finite
+ * gaps below that count in full, however small q_rest is.  An entry whose id is negative is padding (lists of different lengths); one
+ * whose id is not below vocab, or stood in the row before, is left out too and raises TM_DEV_BADID in *status_dev.
  * A row of weight 0, or without entries, has loss 0 and gradient 0 whatever its logits hold.  0 <= k <= TM_TOP_MAX.
- *   tm_distill_loss       loss_out[rows]; stats_out[rows][2] (may be NULL): log-sum-exp of logits / temperature, log q_rest (0 without teacher_lse)
+ *   tm_distill_loss       loss_out[rows]; stats_out[rows][2] (may be NULL): log-sum-exp of logits / temperature, log q_rest (0 without
+ *                         teacher_lse, -Inf without mass there)
  *   tm_distill_grad       dlogits, from the stats of tm_distill_loss on the same arguments, times grad_loss[row] (NULL: 1)
  *   tm_distill_loss_grad  both in one pass over the logits, for a step whose gradient of the loss is known (1 per row; a factor goes into scale)
  * dlogits may lie on logits.

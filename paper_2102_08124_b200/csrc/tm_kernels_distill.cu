@@ -6,8 +6,11 @@
 //   dloss/dz  = f / T (q_j - p_j) for a listed logit,  f / T (q_j - p_rest q_j / q_rest) for another one
 //
 // q_rest is the sum over the unlisted logits themselves, never one minus the listed mass: the difference would lose all its
-// digits where the student puts nearly everything on the list.  Terms with p = 0 are left out, and so is the rest's term where
-// the student has no mass there.
+// digits where the student puts nearly everything on the list.  The unlisted logits' sum has a reference of its own, the largest of them,
+// so that log q_rest is right however far they lie below the listed ones, and an unlisted gradient is written as
+// f / T (q_rest - p_rest) (q_j / q_rest), whose last factor is a softmax over the unlisted logits alone.
+// Terms with p = 0 are left out, and so is the rest's term where the student has no mass there: unlisted logits of -Inf, or more than
+// 2^20 binades below the listed ones, which only masks are.
 #include <algorithm>
 #include <type_traits>
 
@@ -37,9 +40,11 @@ template <bool LOSS> __device__ __forceinline__ float power_of(float z, float R,
     return LOSS ? exp2_fast((z - R) * c2) : exp2_fast(fmaf(z, inv_t, -R) * (float)kLog2eD);
 }
 
-// What a row's gradient needs beside its list: q = 2^(x - R) inv, unlisted logits times off.
-struct Scale { float R, inv, off; bool slow; };
-__device__ __forceinline__ Scale scale_of_stats(float lse, float log_rest, float rest) {
+constexpr float kMasked = 1048576.0f;                    // binades below the listed logits from which unlisted ones count as masked
+
+// What a row's gradient needs beside its list, in units of f / T: 2^(x - R) inv - p for a listed logit, 2^(x - R_rest) rest for another one.
+struct Scale { float R, inv, R_rest, rest; bool slow; };
+__device__ __forceinline__ Scale scale_of_stats(float lse, float log_rest, float p_rest) {
     // q = 2^(x - R) 2^(R - lse log2 e): the second factor, of R's rounding, joins the others
     const double want = (double)lse * kLog2eD;
     Scale k;
@@ -47,7 +52,14 @@ __device__ __forceinline__ Scale scale_of_stats(float lse, float log_rest, float
     k.slow = !(fabsf(k.R) < 1e30f);
     k.inv = k.slow ? 1.0f : exp2f((float)((double)k.R - want));
     if (k.slow) k.R = lse;
-    k.off = rest > 0.0f && log_rest > -INFINITY ? 1.0f - rest * expf(-log_rest) : 1.0f;
+    k.R_rest = k.R;
+    k.rest = k.inv;
+    if (p_rest > 0.0f && log_rest > -kMasked * (float)kLn2D) {
+        // the same for q_j / q_rest, whose logarithm is x less the sum of the two statistics
+        const double lse_rest = (double)lse + log_rest, want_rest = lse_rest * kLog2eD;
+        k.R_rest = k.slow ? (float)lse_rest : (float)want_rest;
+        k.rest = (expf(log_rest) - p_rest) * (k.slow ? 1.0f : exp2f((float)((double)k.R_rest - want_rest)));
+    }
     return k;
 }
 
@@ -165,13 +177,13 @@ __device__ __forceinline__ void fetch_list(const DistillArgs& a, long long r, in
 
 // A row's loss, by one warp: sum p log p - sum p log q + p_rest (log p_rest - log q_rest), put together in 64 bits because the sums
 // nearly cancel.  The four logs are taken side by side in four lanes.  dot: sum p z; lse_shift: what the exponentials' sums are
-// relative to, in units of the temperature.  Lane 0 returns the loss, and the statistics.
-__device__ __forceinline__ float row_loss(float entropy, float mass, float norm, float rest, double dot, double inv_t, double lse_shift, float s_all, float s_rest,
+// relative to, in units of the temperature; gap: how far the rest's reference lies below it.  Lane 0 returns the loss, and the statistics.
+__device__ __forceinline__ float row_loss(float entropy, float mass, float norm, float rest, double dot, double inv_t, double lse_shift, double gap, float s_all, float s_rest,
                                           float& lse, float& log_rest) {
     const int lane = threadIdx.x & 31;
     const double l = log((double)(lane == 0 ? s_all : lane == 1 ? s_rest : lane == 2 ? rest : norm));
     const double log_s = __shfl_sync(0xFFFFFFFFu, l, 1), log_r = __shfl_sync(0xFFFFFFFFu, l, 2), log_n = __shfl_sync(0xFFFFFFFFu, l, 3);
-    const double lse_d = lse_shift + l, log_rest_d = log_s - l;          // lane 0's
+    const double lse_d = lse_shift + l, log_rest_d = log_s - l - gap;    // lane 0's
     double loss = (double)entropy - mass * log_n - dot * inv_t + mass * lse_d;
     if (rest > 0.0f && s_rest > 0.0f) loss += rest * (log_r - log_rest_d);
     if (s_rest != s_rest) loss = s_rest;
@@ -346,10 +358,10 @@ __global__ void __launch_bounds__(NT + 32, kBlocks<LOSS, NT>) distill_kernel(con
         Scale k;
         float rest;
         if constexpr (LOSS) {
-            float s_rest, s_all, m = lowest(), s = 0.0f;
+            float s_rest, s_list, R_rest, R_list, m = lowest(), s = 0.0f;
             double dot = 0.0;
             float entropy = 0.0f, mass = 0.0f, norm = 1.0f;
-            // everybody's (m, s) against the list's: the largest m as R, the sums relative to it
+            // the largest m of the workers' (m, s) and of the lists', each with the sums relative to it
             auto totals = [&]() {
                 const float wm = group_max<32>(m);
                 const float ws = group_sum<32>(s * exp2_fast(m - wm));
@@ -364,14 +376,15 @@ __global__ void __launch_bounds__(NT + 32, kBlocks<LOSS, NT>) distill_kernel(con
                 float top = lowest();
                 for (int i = lane; i < C * NW; i += 32) top = fmaxf(top, (C > 1 ? cluster_load2(&part[turn][i % NW], i / NW) : part[turn][i]).x);
                 if (lane < C) of_list = C > 1 ? cluster_load2(&list_part[turn], lane) : list_part[turn];
-                k.R = group_max<32>(fmaxf(top, of_list.x));
+                R_rest = group_max<32>(top);
+                R_list = group_max<32>(of_list.x);
                 float sum = 0.0f;
                 for (int i = lane; i < C * NW; i += 32) {
                     const float2 v = C > 1 ? cluster_load2(&part[turn][i % NW], i / NW) : part[turn][i];
-                    sum += v.y * exp2_fast(v.x - k.R);
+                    sum += v.y * exp2_fast(v.x - R_rest);
                 }
                 s_rest = group_sum<32>(sum);
-                s_all = s_rest + group_sum<32>(of_list.y * exp2_fast(of_list.x - k.R));
+                s_list = group_sum<32>(of_list.y * exp2_fast(of_list.x - R_list));
                 if (lister && rank == 0) {
                     dot = lane < C ? (C > 1 ? cluster_load_double(&dot_part[turn], lane) : dot_part[turn]) : 0.0;
                     dot = warp_sum_double(dot);
@@ -474,34 +487,43 @@ __global__ void __launch_bounds__(NT + 32, kBlocks<LOSS, NT>) distill_kernel(con
                 s = add.x + add.y;
             }
             totals();
-            k.slow = !(fabsf(k.R) < 1e30f);
+            k.slow = !(fabsf(fmaxf(R_rest, R_list)) < 1e30f);
             if (k.slow) {
-                // logits so large or small that their scaled form leaves the range: the largest one as it is, then the sums
+                // logits so large or small that their scaled form leaves the range: the largest ones as they are, then the sums
                 const double all_dot = dot;
                 m = lowest(); s = 0.0f; dot = 0.0;
                 if (lister) { for (int e = lane; e < slots; e += 32) m = fmaxf(m, list_z[e]); }
                 else { if (blocks > 0) fetch(w, vec, 0); each([&](const uint4 (&now)[U]) { for (int u = 0; u < U; ++u) m = fmaxf(m, vector_max<DT>(now[u])); }, false); }
                 totals();
-                const float M = k.R;
+                const float M_rest = R_rest, M_list = R_list;
                 m = 0.0f; s = 0.0f; dot = 0.0;
-                if (lister) { for (int e = lane; e < slots; e += 32) s += exp2_fast((list_z[e] - M) * c2); }
+                if (lister) { for (int e = lane; e < slots; e += 32) s += exp2_fast((list_z[e] - M_list) * c2); }
                 else {
                     if (blocks > 0) fetch(w, vec, 0);
                     each([&](const uint4 (&now)[U]) {
                         for (int u = 0; u < U; ++u) {
                             float v[V];
                             unpack_vector<DT>(now[u], v);
-                            for (int j = 0; j < V; ++j) s += exp2_fast((v[j] - M) * c2);
+                            for (int j = 0; j < V; ++j) s += exp2_fast((v[j] - M_rest) * c2);
                         }
                     }, false);
                 }
                 totals();
-                k.R = M;
+                R_rest = M_rest; R_list = M_list;
                 dot = all_dot;
             }
             rest = rest_s;
+            const float unit = k.slow ? c2 : 1.0f;        // binades of a difference of references
+            k.R = fmaxf(R_rest, R_list);
+            const float gap = (k.R - R_rest) * unit, s_all = s_rest * exp2_fast(-gap) + s_list * exp2_fast((R_list - k.R) * unit);
+            if (!(gap < kMasked) && s_rest == s_rest) s_rest = 0.0f;
             k.inv = 1.0f / s_all;
-            k.off = rest > 0.0f && s_rest > 0.0f ? 1.0f - rest * s_all / s_rest : 1.0f;
+            k.R_rest = k.R;
+            k.rest = k.inv;
+            if (rest > 0.0f && s_rest > 0.0f) {
+                k.R_rest = R_rest;
+                k.rest = exp2_fast(-gap) * k.inv - rest / s_rest;         // (q_rest - p_rest) / s_rest
+            }
             if (lister) {
                 for (int e = lane; e < slots; e += 32) unflag(e);
                 __syncwarp();
@@ -509,7 +531,8 @@ __global__ void __launch_bounds__(NT + 32, kBlocks<LOSS, NT>) distill_kernel(con
             }
             if (lister && rank == 0) {
                 float lse, log_rest;
-                const float loss = row_loss(entropy, mass, norm, rest, dot, plan.inv_t_d, k.slow ? k.R * plan.inv_t_d : k.R * plan.kappa * kLn2D, s_all, s_rest, lse, log_rest);
+                const float loss = row_loss(entropy, mass, norm, rest, dot, plan.inv_t_d, k.slow ? k.R * plan.inv_t_d : k.R * plan.kappa * kLn2D,
+                                            ((double)k.R - R_rest) * (k.slow ? plan.inv_t_d : plan.kappa * kLn2D), s_all, s_rest, lse, log_rest);
                 if (lane == 0) {
                     a.loss[r] = loss * weight * a.scale;
                     if (!GRAD && a.stats) { a.stats[2 * r] = lse; a.stats[2 * r + 1] = a.teacher_lse ? log_rest : 0.0f; }
@@ -521,11 +544,11 @@ __global__ void __launch_bounds__(NT + 32, kBlocks<LOSS, NT>) distill_kernel(con
             if (lister && r + step < a.rows) fetch_list(a, r + step, slots, list_id, list_v);
         }
         if constexpr (GRAD) {
-            const float up = weight * a.scale * (!LOSS && a.grad_loss ? a.grad_loss[r] : 1.0f) * inv_t, scale = up * k.off * k.inv;
+            const float up = weight * a.scale * (!LOSS && a.grad_loss ? a.grad_loss[r] : 1.0f) * inv_t, scale = up * k.rest;
             if (!lister) {
                 const int kept = LOSS ? plan.stash : 0;
                 if (LOSS && blocks > 0) fetch(w, kept > 0 ? stash : vec, 0);
-                const float2 cc = make_float2(c2, c2), rr = make_float2(-k.R, -k.R), ss = make_float2(scale, scale);
+                const float2 cc = make_float2(c2, c2), rr = make_float2(-k.R_rest, -k.R_rest), ss = make_float2(scale, scale);
                 auto pass = [&](auto&& power2) {
                     walk(kept, [&](uint4 (&now)[U], int b) {
                         const int i0 = b * (NT * U) + tid;
@@ -545,8 +568,8 @@ __global__ void __launch_bounds__(NT + 32, kBlocks<LOSS, NT>) distill_kernel(con
                     });
                 };
                 if (!k.slow) pass([&](float2 z) { const float2 x = __ffma2_rn(z, cc, rr); return make_float2(exp2_fast(x.x), exp2_fast(x.y)); });
-                else pass([&](float2 z) { return make_float2(power_of<LOSS>(z.x, k.R, true, c2, inv_t), power_of<LOSS>(z.y, k.R, true, c2, inv_t)); });
-                if (tid < edges) from_float(out + slice.edge(tid), scale * power_of<LOSS>(to_float(row.base[slice.edge(tid)]), k.R, k.slow, c2, inv_t));
+                else pass([&](float2 z) { return make_float2(power_of<LOSS>(z.x, k.R_rest, true, c2, inv_t), power_of<LOSS>(z.y, k.R_rest, true, c2, inv_t)); });
+                if (tid < edges) from_float(out + slice.edge(tid), scale * power_of<LOSS>(to_float(row.base[slice.edge(tid)]), k.R_rest, k.slow, c2, inv_t));
             }
             __syncthreads();
             if (lister)
