@@ -33,14 +33,14 @@ constexpr int kHash = 512, kEntries = kTopMax / 32;      // slots of the table t
 
 __device__ __forceinline__ float lowest() { return -3.4028234663852886e38f; }
 
-// 2^(x - R) of a logit: `slow` rows (R outside the range in which x = z c2 is safe) have R in logits and take the difference first.
+// 2^(x - R) of a logit: `slow` rows (R out of the reach of scaled differences) have R in logits and take the difference first.
 // LOSS: R from the row's own sums; otherwise from the statistics, a log-sum-exp in units of the temperature.
 template <bool LOSS> __device__ __forceinline__ float power_of(float z, float R, bool slow, float c2, float inv_t) {
     if (!slow) return exp2_fast(fmaf(z, c2, -R));
     return LOSS ? exp2_fast((z - R) * c2) : exp2_fast(fmaf(z, inv_t, -R) * (float)kLog2eD);
 }
 
-constexpr float kMasked = 1048576.0f;                    // binades below the listed logits from which unlisted ones count as masked
+constexpr float kMasked = 1048576.0f;                    // less than kReach above kFloor: binades below the listed logits from which unlisted ones count as masked
 
 // What a row's gradient needs beside its list, in units of f / T: 2^(x - R) inv - p for a listed logit, 2^(x - R_rest) rest for another one.
 struct Scale { float R, inv, R_rest, rest; bool slow; };
@@ -49,7 +49,7 @@ __device__ __forceinline__ Scale scale_of_stats(float lse, float log_rest, float
     const double want = (double)lse * kLog2eD;
     Scale k;
     k.R = (float)want;
-    k.slow = !(fabsf(k.R) < 1e30f);
+    k.slow = !(fabsf(k.R) < kReach);
     k.inv = k.slow ? 1.0f : exp2f((float)((double)k.R - want));
     if (k.slow) k.R = lse;
     k.R_rest = k.R;
@@ -204,7 +204,7 @@ __device__ __forceinline__ float row_loss(float entropy, float mass, float norm,
 //           warp puts the loss together; after the pass it writes the listed logits' gradients.
 // Several blocks share an SM, so one's loads cover another's exponentials and waits.
 // Exponents live in base 2, scaled: x_j = z_j c2 with c2 = log2(e) / T, as differences x_j - R with one rounding (fma), R the largest
-// x.  A row whose R lies outside +-1e30 (all logits masked by the type's lowest value, say) goes again with the difference first.
+// x.  A row whose R is out of their reach (all logits masked, say) goes again with differences of the logits first.
 
 constexpr int kMaxCluster = 8;
 constexpr size_t kRowSmem = 216 * 1024;            // of a block's 227 KB, beside the static arrays
@@ -358,7 +358,7 @@ __global__ void __launch_bounds__(NT + 32, kBlocks<LOSS, NT>) distill_kernel(con
         Scale k;
         float rest;
         if constexpr (LOSS) {
-            float s_rest, s_list, R_rest, R_list, m = lowest(), s = 0.0f;
+            float s_rest, s_list, R_rest, R_list, m = kFloor, s = 0.0f;
             double dot = 0.0;
             float entropy = 0.0f, mass = 0.0f, norm = 1.0f;
             // the largest m of the workers' (m, s) and of the lists', each with the sums relative to it
@@ -487,9 +487,9 @@ __global__ void __launch_bounds__(NT + 32, kBlocks<LOSS, NT>) distill_kernel(con
                 s = add.x + add.y;
             }
             totals();
-            k.slow = !(fabsf(fmaxf(R_rest, R_list)) < 1e30f);
+            k.slow = !(fabsf(fmaxf(R_rest, R_list)) < kReach);
             if (k.slow) {
-                // logits so large or small that their scaled form leaves the range: the largest ones as they are, then the sums
+                // the largest logit lies out of reach of scaled differences: the largest ones as they are, then the sums
                 const double all_dot = dot;
                 m = lowest(); s = 0.0f; dot = 0.0;
                 if (lister) { for (int e = lane; e < slots; e += 32) m = fmaxf(m, list_z[e]); }

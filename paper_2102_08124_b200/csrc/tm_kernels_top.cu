@@ -228,7 +228,7 @@ template <int DT, int NT> __global__ void __launch_bounds__(NT, kBlocks<NT>) top
                 use(w, b);
             }
         };
-        float m = -3.4028234663852886e38f, s = 0.0f, largest = -INFINITY;
+        float m = kFloor, s = 0.0f, largest = -INFINITY;
         walk(0, [&](const uint4 (&w)[U], int b) {
             if (b < plan.stash) {
 #pragma unroll
@@ -357,12 +357,12 @@ template <int DT, int NT> __global__ void __launch_bounds__(NT, kBlocks<NT>) top
             if (a.lse && !finite) a.lse[r] = M;
         }
         if (a.lse && finite) {
-            float R = -3.4028234663852886e38f;
+            float R = kFloor;
             for (int i = lane; i < C * NW; i += 32) R = fmaxf(R, part_of(i).x);
             R = group_max<32>(R);
-            const bool slow = !(fabsf(R) < 1e30f);
+            const bool slow = !(fabsf(R) < kReach);
             if (slow) {
-                // logits so large or small that their scaled form leaves the range: again, with the difference first
+                // the largest logit lies out of reach of scaled differences: again, with the difference first
                 s = 0.0f;
                 auto add = [&](float v) { s += exp2_fast((v - M) * c2); };
                 for (int i = tid; i < inside; i += NT) {

@@ -135,6 +135,12 @@ template <int DT> struct RowPart {
     __device__ __forceinline__ long long edge(int k) const { return k < head ? column - head + k : column + (long long)inside * V + (k - head); }
 };
 
+// Softmax sums take 2^(x - m) of scaled logits x = z log2(e) / T as fma(z, log2(e) / T, -m), m the running maximum of the rounded x.  The
+// difference then holds that rounding, half a unit of m's last place: below one binade up to 2^24, but past 2^31 more than fp32's
+// range.  So m starts at kFloor and what lies below it (masks, beside ordinary logits) counts as zero; a row whose largest x is not inside
+// +-kReach goes again with differences of the logits themselves.
+constexpr float kFloor = -16777216.0f, kReach = 8388608.0f;
+
 // 2^x, flushed to zero below the normal range: one instruction, relative error below 2^-22
 __device__ __forceinline__ float exp2_fast(float x) {
     float y;

@@ -37,7 +37,7 @@ def _formula(z, v, ids, lse_t, t, scale):
 
 
 def _run(z, v, ids, lse, t, scale):
-    dev = lambda a: torch.from_numpy(np.ascontiguousarray(a)).cuda()
+    dev = lambda a: None if a is None else torch.from_numpy(np.ascontiguousarray(a)).cuda()
     kw = dict(teacher_lse=dev(lse), temperature=t, scale=scale)
     loss, stats = tm.tm_distill_loss(z, dev(v), dev(ids), **kw)
     grad = tm.tm_distill_grad(z, dev(v), dev(ids), stats, **kw)
