@@ -67,7 +67,7 @@ __device__ __forceinline__ Scale scale_of_stats(float lse, float log_rest, float
 struct List {
     int id[kEntries];
     float p[kEntries];     // the teacher's probability (its logit until probabilities() ran)
-    float entropy, mass;   // sum p (log p + log norm), sum p
+    float entropy;         // sum p (log p + log norm)
     float norm;            // what the exponentials were divided by (1 where the teacher's log-sum-exp is given)
     float rest;            // p_rest
     bool some;             // any entry
@@ -130,7 +130,8 @@ struct List {
     __device__ __forceinline__ void probabilities(const DistillArgs& a, float weight, float lse_t, float it, float it_low) {
         float top = -INFINITY;
         some = false;
-        entropy = mass = rest = 0.0f;
+        float mass = 0.0f;
+        entropy = rest = 0.0f;
         norm = 1.0f;
 #pragma unroll
         for (int e = 0; e < kEntries; ++e)
@@ -154,7 +155,6 @@ struct List {
         if (own) {
             norm = mass;
             scale = 1.0f / norm;
-            mass = 1.0f;
         } else rest = fmaxf(0.0f, 1.0f - mass);
 #pragma unroll
         for (int e = 0; e < kEntries; ++e) {
@@ -175,19 +175,29 @@ __device__ __forceinline__ void fetch_list(const DistillArgs& a, long long r, in
     __syncwarp();
 }
 
+// What a block's listed logits add to the loss: sum p and sum p (z - z0), z0 the largest of them.  entropy, norm: the list's.
+struct ListSums { double mass, dot; float z0, entropy, norm; };
+
 // A row's loss, by one warp: sum p log p - sum p log q + p_rest (log p_rest - log q_rest), put together in 64 bits because the sums
-// nearly cancel.  The four logs are taken side by side in four lanes.  dot: sum p z; lse_shift: what the exponentials' sums are
-// relative to, in units of the temperature; gap: how far the rest's reference lies below it.  Lane 0 returns the loss, and the statistics.
-__device__ __forceinline__ float row_loss(float entropy, float mass, float norm, float rest, double dot, double inv_t, double lse_shift, double gap, float s_all, float s_rest,
-                                          float& lse, float& log_rest) {
+// nearly cancel: an offset that all logits share drops out of (z0 - R) before anything is rounded.  Lane c brings block c's ListSums (zeros
+// from C on; entropy and norm: those of any block).  The four logs are taken side by side in four lanes.  base: what the exponentials' sums are relative to, in units of the
+// temperature -- R base_unit, or R itself where `slow` -- and gap: how far the rest's reference lies below it.  Lane 0 returns the loss,
+// and the statistics.
+__device__ __forceinline__ float row_loss(float rest, const ListSums& l, bool slow, double inv_t, double base_unit, float R, float R_rest, float s_all,
+                                          float s_rest, float& lse, float& log_rest) {
     const int lane = threadIdx.x & 31;
-    const double l = log((double)(lane == 0 ? s_all : lane == 1 ? s_rest : lane == 2 ? rest : norm));
-    const double log_s = __shfl_sync(0xFFFFFFFFu, l, 1), log_r = __shfl_sync(0xFFFFFFFFu, l, 2), log_n = __shfl_sync(0xFFFFFFFFu, l, 3);
-    const double lse_d = lse_shift + l, log_rest_d = log_s - l - gap;    // lane 0's
-    double loss = (double)entropy - mass * log_n - dot * inv_t + mass * lse_d;
+    const double unit = slow ? inv_t : base_unit;
+    const double mass = warp_sum_double(l.mass);
+    const double above = slow ? ((double)l.z0 - R) * inv_t : l.z0 * inv_t - R * base_unit;       // z0 / T - base
+    const double cross = warp_sum_double(l.dot * inv_t + (l.mass > 0.0 ? l.mass * above : 0.0));  // sum p (z / T - base)
+    const double g = log((double)(lane == 0 ? s_all : lane == 1 ? s_rest : lane == 2 ? rest : l.norm));
+    const double log_all = __shfl_sync(0xFFFFFFFFu, g, 0), log_s = __shfl_sync(0xFFFFFFFFu, g, 1), log_r = __shfl_sync(0xFFFFFFFFu, g, 2),
+                 log_n = __shfl_sync(0xFFFFFFFFu, g, 3);
+    const double log_rest_d = log_s - log_all - ((double)R - R_rest) * unit;
+    double loss = (double)__shfl_sync(0xFFFFFFFFu, l.entropy, 0) - mass * log_n - cross + mass * log_all;
     if (rest > 0.0f && s_rest > 0.0f) loss += rest * (log_r - log_rest_d);
     if (s_rest != s_rest) loss = s_rest;
-    lse = (float)lse_d;
+    lse = (float)(R * unit + log_all);
     log_rest = (float)log_rest_d;
     return (float)loss;
 }
@@ -235,7 +245,7 @@ __global__ void __launch_bounds__(NT + 32, kBlocks<LOSS, NT>) distill_kernel(con
     __shared__ int list_at[kTopMax];                                      // ids of this slice's listed logits, or -1
     __shared__ float list_p[kTopMax], list_z[kTopMax];
     __shared__ float2 part[2][NW], list_part[2];
-    __shared__ double dot_part[2];
+    __shared__ ListSums list_sums[2];
     __shared__ float rest_s;
     __shared__ int on_s;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -359,15 +369,12 @@ __global__ void __launch_bounds__(NT + 32, kBlocks<LOSS, NT>) distill_kernel(con
         float rest;
         if constexpr (LOSS) {
             float s_rest, s_list, R_rest, R_list, m = kFloor, s = 0.0f;
-            double dot = 0.0;
-            float entropy = 0.0f, mass = 0.0f, norm = 1.0f;
             // the largest m of the workers' (m, s) and of the lists', each with the sums relative to it
             auto totals = [&]() {
                 const float wm = group_max<32>(m);
                 const float ws = group_sum<32>(s * exp2_fast(m - wm));
-                if (lister) dot = warp_sum_double(dot);
                 if (lane == 0) {
-                    if (lister) { list_part[turn] = make_float2(wm, ws); dot_part[turn] = dot; }
+                    if (lister) list_part[turn] = make_float2(wm, ws);
                     else part[turn][warp] = make_float2(wm, ws);
                 }
                 __syncwarp();
@@ -385,10 +392,6 @@ __global__ void __launch_bounds__(NT + 32, kBlocks<LOSS, NT>) distill_kernel(con
                 }
                 s_rest = group_sum<32>(sum);
                 s_list = group_sum<32>(of_list.y * exp2_fast(of_list.x - R_list));
-                if (lister && rank == 0) {
-                    dot = lane < C ? (C > 1 ? cluster_load_double(&dot_part[turn], lane) : dot_part[turn]) : 0.0;
-                    dot = warp_sum_double(dot);
-                }
                 turn ^= 1;
             };
             // listed elements of a vector become -Inf
@@ -443,8 +446,7 @@ __global__ void __launch_bounds__(NT + 32, kBlocks<LOSS, NT>) distill_kernel(con
                 List list;
                 list.load(list_id, list_v, slots);
                 list.probabilities(a, weight, a.teacher_lse ? a.teacher_lse[r] : 0.0f, inv_t, plan.inv_t_low);
-                entropy = list.entropy; mass = list.mass; norm = list.norm;
-                float z[kEntries];
+                float z[kEntries], z0 = -INFINITY;
 #pragma unroll
                 for (int e = 0; e < kEntries; ++e) {
                     if (e * 32 >= slots) break;
@@ -452,15 +454,24 @@ __global__ void __launch_bounds__(NT + 32, kBlocks<LOSS, NT>) distill_kernel(con
                     z[e] = id >= 0 ? to_float(row.base[id]) : -INFINITY;
                     list_p[e * 32 + lane] = list.p[e];
                     list_z[e * 32 + lane] = z[e];
-                    m = fmaxf(m, z[e] * c2);
-                    if (id >= 0 && list.p[e] != 0.0f) dot += (double)list.p[e] * z[e];
+                    z0 = fmaxf(z0, z[e]);
                 }
+                m = fmaxf(m, z0 * c2);
+                z0 = group_max<32>(z0);
+                if (!(z0 > -INFINITY)) z0 = 0.0f;
+                double mass = 0.0, dot = 0.0;
 #pragma unroll
                 for (int e = 0; e < kEntries; ++e) {
                     if (e * 32 >= slots) break;
                     s += exp2_fast(fmaf(z[e], c2, -m));
+                    if (list_at[e * 32 + lane] >= 0 && list.p[e] != 0.0f) {
+                        mass += list.p[e];
+                        dot += (double)list.p[e] * ((double)z[e] - z0);
+                    }
                 }
-                if (lane == 0) rest_s = list.rest;
+                mass = warp_sum_double(mass);
+                dot = warp_sum_double(dot);
+                if (lane == 0) { rest_s = list.rest; list_sums[turn] = {mass, dot, z0, list.entropy, list.norm}; }
             } else {
                 float2 add = make_float2(0.0f, 0.0f);
                 const float2 cc = make_float2(c2, c2);
@@ -490,13 +501,12 @@ __global__ void __launch_bounds__(NT + 32, kBlocks<LOSS, NT>) distill_kernel(con
             k.slow = !(fabsf(fmaxf(R_rest, R_list)) < kReach);
             if (k.slow) {
                 // the largest logit lies out of reach of scaled differences: the largest ones as they are, then the sums
-                const double all_dot = dot;
-                m = lowest(); s = 0.0f; dot = 0.0;
+                m = lowest(); s = 0.0f;
                 if (lister) { for (int e = lane; e < slots; e += 32) m = fmaxf(m, list_z[e]); }
                 else { if (blocks > 0) fetch(w, vec, 0); each([&](const uint4 (&now)[U]) { for (int u = 0; u < U; ++u) m = fmaxf(m, vector_max<DT>(now[u])); }, false); }
                 totals();
                 const float M_rest = R_rest, M_list = R_list;
-                m = 0.0f; s = 0.0f; dot = 0.0;
+                m = 0.0f; s = 0.0f;
                 if (lister) { for (int e = lane; e < slots; e += 32) s += exp2_fast((list_z[e] - M_list) * c2); }
                 else {
                     if (blocks > 0) fetch(w, vec, 0);
@@ -510,7 +520,6 @@ __global__ void __launch_bounds__(NT + 32, kBlocks<LOSS, NT>) distill_kernel(con
                 }
                 totals();
                 R_rest = M_rest; R_list = M_list;
-                dot = all_dot;
             }
             rest = rest_s;
             const float unit = k.slow ? c2 : 1.0f;        // binades of a difference of references
@@ -531,8 +540,16 @@ __global__ void __launch_bounds__(NT + 32, kBlocks<LOSS, NT>) distill_kernel(con
             }
             if (lister && rank == 0) {
                 float lse, log_rest;
-                const float loss = row_loss(entropy, mass, norm, rest, dot, plan.inv_t_d, k.slow ? k.R * plan.inv_t_d : k.R * plan.kappa * kLn2D,
-                                            ((double)k.R - R_rest) * (k.slow ? plan.inv_t_d : plan.kappa * kLn2D), s_all, s_rest, lse, log_rest);
+                const ListSums* const sums = &list_sums[turn ^ 1];        // as turn was in pass 1: one round of totals, or three
+                ListSums l = *sums;
+                if (C > 1) {
+                    const uint32_t c = lane < C ? lane : 0;
+                    l.mass = cluster_load_double(&sums->mass, c);
+                    l.dot = cluster_load_double(&sums->dot, c);
+                    l.z0 = cluster_load_float(&sums->z0, c);
+                }
+                if (lane >= C) l.mass = l.dot = 0.0;
+                const float loss = row_loss(rest, l, k.slow, plan.inv_t_d, plan.kappa * kLn2D, k.R, R_rest, s_all, s_rest, lse, log_rest);
                 if (lane == 0) {
                     a.loss[r] = loss * weight * a.scale;
                     if (!GRAD && a.stats) { a.stats[2 * r] = lse; a.stats[2 * r + 1] = a.teacher_lse ? log_rest : 0.0f; }

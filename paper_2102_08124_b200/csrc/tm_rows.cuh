@@ -211,6 +211,11 @@ __device__ __forceinline__ float2 cluster_load2(const float2* shared, uint32_t r
     asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(cluster_map(shared, rank)) : "memory");
     return v;
 }
+__device__ __forceinline__ float cluster_load_float(const float* shared, uint32_t rank) {
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(cluster_map(shared, rank)) : "memory");
+    return v;
+}
 __device__ __forceinline__ unsigned long long cluster_load64(const unsigned long long* shared, uint32_t rank) {
     unsigned long long v;
     asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(cluster_map(shared, rank)) : "memory");

@@ -56,3 +56,50 @@ def test_masked_logits_outside_the_list_are_no_mass(tail, vocab, t, dtype):
     assert np.isfinite(results[0][0]).all() and np.isfinite(results[0][3]).all() and np.isfinite(results[0][4]).all()
     for other in results[1:]:
         assert all(np.array_equal(a, b) for a, b in zip(results[0], other))
+
+
+def _offset_rows(rng, vocab, k, offset, dtype, spread):
+    """Rows whose logits are small multiples of 1/16 plus an offset that keeps them exact; the rows without it."""
+    z = np.round(rng.standard_normal((3, vocab)) * spread * 16) / 16
+    ids = np.stack([rng.permutation(vocab)[:k] for _ in range(3)]).astype(np.int32)
+    host = torch.from_numpy((z + offset).astype(np.float32)).to(DT[dtype])
+    assert np.array_equal(host.double().numpy() - offset, z)
+    return host.cuda(), z, ids, rng.standard_normal((3, k)).astype(np.float32) + 2
+
+
+def _shared_offset(offset, spread, vocab, t, tail, dtype, outputs):
+    """An offset that all logits share changes neither loss nor gradient: the bounds are those of the rows without it."""
+    rng = np.random.Generator(np.random.PCG64(abs(int(min(offset, 1e6))) + vocab))
+    k, scale = 24, 1.5
+    z, zd, ids, v = _offset_rows(rng, vocab, k, offset, dtype, spread)
+    lse_t = np.array([ref.log_sum_exp(x.astype(np.float64) / t) + 0.25 for x in v], np.float32) if tail else None
+    loss, loss2, stats, grad, grad2 = _run(z, v, ids, lse_t, t, scale)
+    for r in range(3):
+        want, dz, lse, _, (bl, bg) = ref.distill(zd[r], v[r].astype(np.float64), ids[r], float(lse_t[r]) if tail else None, 1.0, t, scale)
+        assert abs(loss[r] - want) <= bl and abs(loss2[r] - want) <= bl, (r, loss[r], loss2[r], want, bl)
+        shifted = lse + offset / t
+        with np.errstate(over="ignore"):
+            rounded = np.float32(shifted)
+        assert stats[r, 0] == rounded or abs(stats[r, 0] - shifted) <= 4 * ref.sum_unit(vocab, abs(lse)) + 2 * ref.U32 * abs(shifted)   # (it may be past fp32's range)
+        bound = 2 * bg + (ref.out_unit(dtype) + 4 * ref.U32) * np.abs(dz) + 2.0 ** -126 * (1 + scale / t)      # exponentials below the normal range are zero
+        for name, g in (("both", grad2), ("grad", grad)):
+            wrong = ~(np.abs(g[r] - dz) <= bound)
+            assert name not in outputs or not wrong.any(), (r, name, wrong.sum(), np.flatnonzero(wrong)[:4], g[r][wrong][:4], dz[wrong][:4])
+
+
+@pytest.mark.parametrize("tail", [False, True])
+@pytest.mark.parametrize("t", [1.0, 0.0625, 3.0])                                        # 0.0625: scaled differences do not reach the larger offsets
+@pytest.mark.parametrize("vocab", [40, 4001, 70000])
+@pytest.mark.parametrize("offset", [0.0, 600.0, -4096.0, 2.0 ** 18, -2.0 ** 19])
+def test_an_offset_that_all_logits_share(offset, vocab, t, tail):
+    _shared_offset(offset, 1.5, vocab, t, tail, "f32", ("both",))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("tail", [False, True])
+@pytest.mark.parametrize("t", [1.0, 0.5, 3.0])
+@pytest.mark.parametrize("vocab", [40, 4001, 70000])
+@pytest.mark.parametrize("offset", [-2.0 ** 33, 2.0 ** 40, -2.0 ** 100, -2.0 ** 127])
+def test_rows_of_one_level(offset, vocab, t, tail, dtype):
+    """A row that is masked from end to end is a uniform one."""
+    _shared_offset(offset, 0.0, vocab, t, tail, dtype, ("both",))
