@@ -34,33 +34,97 @@ constexpr int kHash = 512, kEntries = kTopMax / 32;      // slots of the table t
 __device__ __forceinline__ float lowest() { return -3.4028234663852886e38f; }
 
 // 2^(x - R) of a logit: `slow` rows (R out of the reach of scaled differences) have R in logits and take the difference first.
-// LOSS: R from the row's own sums; otherwise from the statistics, a log-sum-exp in units of the temperature.
-template <bool LOSS> __device__ __forceinline__ float power_of(float z, float R, bool slow, float c2, float inv_t) {
-    if (!slow) return exp2_fast(fmaf(z, c2, -R));
-    return LOSS ? exp2_fast((z - R) * c2) : exp2_fast(fmaf(z, inv_t, -R) * (float)kLog2eD);
-}
+__device__ __forceinline__ float power_of(float z, float R, bool slow, float c2) { return exp2_fast(slow ? (z - R) * c2 : fmaf(z, c2, -R)); }
 
 constexpr float kMasked = 1048576.0f;                    // less than kReach above kFloor: binades below the listed logits from which unlisted ones count as masked
 
 // What a row's gradient needs beside its list, in units of f / T: 2^(x - R) inv - p for a listed logit, 2^(x - R_rest) rest for another one.
 struct Scale { float R, inv, R_rest, rest; bool slow; };
-__device__ __forceinline__ Scale scale_of_stats(float lse, float log_rest, float p_rest) {
-    // q = 2^(x - R) 2^(R - lse log2 e): the second factor, of R's rounding, joins the others
-    const double want = (double)lse * kLog2eD;
+// The sums of a row: over the unlisted and the listed logits, each relative to the largest of them.
+struct Sums { float R_rest, s_rest, R_list, s_list; };
+// s_rest becomes 0 where the unlisted logits count as masked.  Returns the sum over the whole row, relative to the R that it sets.
+__device__ __forceinline__ float scale_of_sums(Sums& s, float p_rest, bool slow, float c2, Scale& k) {
+    const float unit = slow ? c2 : 1.0f;                  // binades of a difference of references
+    k.slow = slow;
+    k.R = fmaxf(s.R_rest, s.R_list);
+    const float gap = (k.R - s.R_rest) * unit, s_all = s.s_rest * exp2_fast(-gap) + s.s_list * exp2_fast((s.R_list - k.R) * unit);
+    if (!(gap < kMasked) && s.s_rest == s.s_rest) s.s_rest = 0.0f;
+    k.inv = 1.0f / s_all;
+    k.R_rest = k.R;
+    k.rest = k.inv;
+    if (p_rest > 0.0f && s.s_rest > 0.0f) {
+        k.R_rest = s.R_rest;
+        k.rest = exp2_fast(-gap) * k.inv - p_rest / s.s_rest;                  // (q_rest - p_rest) / s_rest
+    }
+    return s_all;
+}
+// The same from the statistics.  unit: what a log-sum-exp in units of T is in scaled logits x = z c2, that is c2 T (log2(e) but for c2's rounding).
+__device__ __forceinline__ Scale scale_of_stats(float lse, float log_rest, float p_rest, double unit) {
+    // q = 2^(x - R) 2^(R - lse unit): the second factor, of R's rounding, joins the others
+    const double want = (double)lse * unit;
     Scale k;
+    k.slow = false;
     k.R = (float)want;
-    k.slow = !(fabsf(k.R) < kReach);
-    k.inv = k.slow ? 1.0f : exp2f((float)((double)k.R - want));
-    if (k.slow) k.R = lse;
+    k.inv = exp2f((float)((double)k.R - want));
     k.R_rest = k.R;
     k.rest = k.inv;
     if (p_rest > 0.0f && log_rest > -kMasked * (float)kLn2D) {
         // the same for q_j / q_rest, whose logarithm is x less the sum of the two statistics
-        const double lse_rest = (double)lse + log_rest, want_rest = lse_rest * kLog2eD;
-        k.R_rest = k.slow ? (float)lse_rest : (float)want_rest;
-        k.rest = (expf(log_rest) - p_rest) * (k.slow ? 1.0f : exp2f((float)((double)k.R_rest - want_rest)));
+        const double want_rest = ((double)lse + log_rest) * unit;
+        k.R_rest = (float)want_rest;
+        k.rest = (expf(log_rest) - p_rest) * exp2f((float)((double)k.R_rest - want_rest));
     }
     return k;
+}
+
+// A log-sum-exp in fp32 is off by up to 2^-24 of itself, and so are then all q = exp(z / T - lse), relatively: beyond this one (2^-14) a row's
+// sums are taken again from its logits.
+constexpr float kFarLse = 1024.0f;
+
+// The sums of a whole row in logits, by all threads of a block; listed logits are told by their ids in the table (kHash words of -1, left
+// so).  For the few rows whose statistics are not enough.
+template <int DT, int THREADS> __device__ __noinline__ Sums sums_of_row(const typename RowType<DT>::T* base, int n, const int* ids, int slots, int* hash, float c2, Sums* part) {
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const auto slot_of = [](int id) { return (int)(((uint32_t)id * 2654435769u) >> 23); };
+    for (int i = tid; i < slots; i += THREADS) {
+        const int id = ids[i];
+        if (id >= 0 && id < n) {
+            int h = slot_of(id);
+            for (int probe = 0; probe < kHash; ++probe, h = (h + 1) & (kHash - 1)) {
+                const int old = atomicCAS(&hash[h], -1, id);
+                if (old == -1 || old == id) break;
+            }
+        }
+    }
+    __syncthreads();
+    float2 sum[2] = {make_float2(lowest(), 0.0f), make_float2(lowest(), 0.0f)};            // unlisted, listed: the largest logit, the sum relative to it
+    const auto add = [&](float2& a, float v) {
+        if (v > a.x) a = make_float2(v, fmaf(a.y, exp2_fast((a.x - v) * c2), 1.0f));
+        else a.y += exp2_fast((v - a.x) * c2);
+    };
+    for (int c = tid; c < n; c += THREADS) {
+        int h = slot_of(c);
+        while (hash[h] != -1 && hash[h] != c) h = (h + 1) & (kHash - 1);                  // at most kTopMax of the kHash words are taken
+        if (hash[h] == c) add(sum[1], to_float(base[c]));
+        else add(sum[0], to_float(base[c]));
+    }
+    Sums s;
+    s.R_rest = group_max<32>(sum[0].x);
+    s.R_list = group_max<32>(sum[1].x);
+    s.s_rest = group_sum<32>(sum[0].y * exp2_fast((sum[0].x - s.R_rest) * c2));
+    s.s_list = group_sum<32>(sum[1].y * exp2_fast((sum[1].x - s.R_list) * c2));
+    if (lane == 0) part[warp] = s;
+    __syncthreads();
+    for (int i = tid; i < kHash; i += THREADS) hash[i] = -1;
+    for (int i = 0; i < THREADS / 32; ++i) { s.R_rest = fmaxf(s.R_rest, part[i].R_rest); s.R_list = fmaxf(s.R_list, part[i].R_list); }
+    s.s_rest = s.s_list = 0.0f;
+    for (int i = 0; i < THREADS / 32; ++i) {
+        s.s_rest += part[i].s_rest * exp2_fast((part[i].R_rest - s.R_rest) * c2);
+        s.s_list += part[i].s_list * exp2_fast((part[i].R_list - s.R_list) * c2);
+    }
+    if (!(fmaxf(s.R_rest, s.R_list) < INFINITY)) s.s_rest = s.s_list = __uint_as_float(0x7FC00000u);
+    __syncthreads();
+    return s;
 }
 
 // A row's list, entry e * 32 + lane in the lanes of one warp: unusable entries (padding, out of range, repeated) get id -1.
@@ -224,7 +288,7 @@ struct RowPlan {
     int slice_vectors, flags;      // flags: bytes, a multiple of 16 (0 without a loss)
     int stash;                     // blocks of NT * U vectors that stay in shared memory between the passes
     float inv_t, inv_t_low, c2;    // 1 / T and what its rounding left out; log2(e) / T
-    double inv_t_d, kappa;         // 1 / T; (log2(e) / T) / c2, the rounding of c2
+    double inv_t_d, kappa, unit;   // 1 / T; (log2(e) / T) / c2, the rounding of c2; c2 T
 };
 
 constexpr int kBlockVectors = 4;                   // vectors of a thread's block
@@ -246,6 +310,7 @@ __global__ void __launch_bounds__(NT + 32, kBlocks<LOSS, NT>) distill_kernel(con
     __shared__ float list_p[kTopMax], list_z[kTopMax];
     __shared__ float2 part[2][NW], list_part[2];
     __shared__ ListSums list_sums[2];
+    __shared__ Sums far_part[NW + 1];
     __shared__ float rest_s;
     __shared__ int on_s;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -368,7 +433,8 @@ __global__ void __launch_bounds__(NT + 32, kBlocks<LOSS, NT>) distill_kernel(con
         Scale k;
         float rest;
         if constexpr (LOSS) {
-            float s_rest, s_list, R_rest, R_list, m = kFloor, s = 0.0f;
+            Sums sums;
+            float m = kFloor, s = 0.0f;
             // the largest m of the workers' (m, s) and of the lists', each with the sums relative to it
             auto totals = [&]() {
                 const float wm = group_max<32>(m);
@@ -383,15 +449,15 @@ __global__ void __launch_bounds__(NT + 32, kBlocks<LOSS, NT>) distill_kernel(con
                 float top = lowest();
                 for (int i = lane; i < C * NW; i += 32) top = fmaxf(top, (C > 1 ? cluster_load2(&part[turn][i % NW], i / NW) : part[turn][i]).x);
                 if (lane < C) of_list = C > 1 ? cluster_load2(&list_part[turn], lane) : list_part[turn];
-                R_rest = group_max<32>(top);
-                R_list = group_max<32>(of_list.x);
+                sums.R_rest = group_max<32>(top);
+                sums.R_list = group_max<32>(of_list.x);
                 float sum = 0.0f;
                 for (int i = lane; i < C * NW; i += 32) {
                     const float2 v = C > 1 ? cluster_load2(&part[turn][i % NW], i / NW) : part[turn][i];
-                    sum += v.y * exp2_fast(v.x - R_rest);
+                    sum += v.y * exp2_fast(v.x - sums.R_rest);
                 }
-                s_rest = group_sum<32>(sum);
-                s_list = group_sum<32>(of_list.y * exp2_fast(of_list.x - R_list));
+                sums.s_rest = group_sum<32>(sum);
+                sums.s_list = group_sum<32>(of_list.y * exp2_fast(of_list.x - sums.R_list));
                 turn ^= 1;
             };
             // listed elements of a vector become -Inf
@@ -498,14 +564,14 @@ __global__ void __launch_bounds__(NT + 32, kBlocks<LOSS, NT>) distill_kernel(con
                 s = add.x + add.y;
             }
             totals();
-            k.slow = !(fabsf(fmaxf(R_rest, R_list)) < kReach);
-            if (k.slow) {
+            const bool slow = !(fabsf(fmaxf(sums.R_rest, sums.R_list)) < kReach);
+            if (slow) {
                 // the largest logit lies out of reach of scaled differences: the largest ones as they are, then the sums
                 m = lowest(); s = 0.0f;
                 if (lister) { for (int e = lane; e < slots; e += 32) m = fmaxf(m, list_z[e]); }
                 else { if (blocks > 0) fetch(w, vec, 0); each([&](const uint4 (&now)[U]) { for (int u = 0; u < U; ++u) m = fmaxf(m, vector_max<DT>(now[u])); }, false); }
                 totals();
-                const float M_rest = R_rest, M_list = R_list;
+                const float M_rest = sums.R_rest, M_list = sums.R_list;
                 m = 0.0f; s = 0.0f;
                 if (lister) { for (int e = lane; e < slots; e += 32) s += exp2_fast((list_z[e] - M_list) * c2); }
                 else {
@@ -519,20 +585,10 @@ __global__ void __launch_bounds__(NT + 32, kBlocks<LOSS, NT>) distill_kernel(con
                     }, false);
                 }
                 totals();
-                R_rest = M_rest; R_list = M_list;
+                sums.R_rest = M_rest; sums.R_list = M_list;
             }
             rest = rest_s;
-            const float unit = k.slow ? c2 : 1.0f;        // binades of a difference of references
-            k.R = fmaxf(R_rest, R_list);
-            const float gap = (k.R - R_rest) * unit, s_all = s_rest * exp2_fast(-gap) + s_list * exp2_fast((R_list - k.R) * unit);
-            if (!(gap < kMasked) && s_rest == s_rest) s_rest = 0.0f;
-            k.inv = 1.0f / s_all;
-            k.R_rest = k.R;
-            k.rest = k.inv;
-            if (rest > 0.0f && s_rest > 0.0f) {
-                k.R_rest = R_rest;
-                k.rest = exp2_fast(-gap) * k.inv - rest / s_rest;         // (q_rest - p_rest) / s_rest
-            }
+            const float s_all = scale_of_sums(sums, rest, slow, c2, k);
             if (lister) {
                 for (int e = lane; e < slots; e += 32) unflag(e);
                 __syncwarp();
@@ -540,16 +596,16 @@ __global__ void __launch_bounds__(NT + 32, kBlocks<LOSS, NT>) distill_kernel(con
             }
             if (lister && rank == 0) {
                 float lse, log_rest;
-                const ListSums* const sums = &list_sums[turn ^ 1];        // as turn was in pass 1: one round of totals, or three
-                ListSums l = *sums;
+                const ListSums* const from = &list_sums[turn ^ 1];        // as turn was in pass 1: one round of totals, or three
+                ListSums l = *from;
                 if (C > 1) {
                     const uint32_t c = lane < C ? lane : 0;
-                    l.mass = cluster_load_double(&sums->mass, c);
-                    l.dot = cluster_load_double(&sums->dot, c);
-                    l.z0 = cluster_load_float(&sums->z0, c);
+                    l.mass = cluster_load_double(&from->mass, c);
+                    l.dot = cluster_load_double(&from->dot, c);
+                    l.z0 = cluster_load_float(&from->z0, c);
                 }
                 if (lane >= C) l.mass = l.dot = 0.0;
-                const float loss = row_loss(rest, l, k.slow, plan.inv_t_d, plan.kappa * kLn2D, k.R, R_rest, s_all, s_rest, lse, log_rest);
+                const float loss = row_loss(rest, l, k.slow, plan.inv_t_d, plan.kappa * kLn2D, k.R, sums.R_rest, s_all, sums.s_rest, lse, log_rest);
                 if (lane == 0) {
                     a.loss[r] = loss * weight * a.scale;
                     if (!GRAD && a.stats) { a.stats[2 * r] = lse; a.stats[2 * r + 1] = a.teacher_lse ? log_rest : 0.0f; }
@@ -557,7 +613,13 @@ __global__ void __launch_bounds__(NT + 32, kBlocks<LOSS, NT>) distill_kernel(con
             }
         } else {
             rest = rest_s;
-            k = scale_of_stats(a.stats[2 * r], a.stats[2 * r + 1], rest);
+            const float lse = a.stats[2 * r];
+            if (fabsf(lse) < kFarLse) k = scale_of_stats(lse, a.stats[2 * r + 1], rest, plan.unit);
+            else {
+                Sums sums = sums_of_row<DT, NT + 32>(row.base, (int)a.vocab, list_id, slots, hash, c2, far_part);
+                scale_of_sums(sums, rest, true, c2, k);
+                if (C > 1) cluster_sync();                // dlogits may be the logits, of which every block has read the whole row
+            }
             if (lister && r + step < a.rows) fetch_list(a, r + step, slots, list_id, list_v);
         }
         if constexpr (GRAD) {
@@ -585,13 +647,13 @@ __global__ void __launch_bounds__(NT + 32, kBlocks<LOSS, NT>) distill_kernel(con
                     });
                 };
                 if (!k.slow) pass([&](float2 z) { const float2 x = __ffma2_rn(z, cc, rr); return make_float2(exp2_fast(x.x), exp2_fast(x.y)); });
-                else pass([&](float2 z) { return make_float2(power_of<LOSS>(z.x, k.R_rest, true, c2, inv_t), power_of<LOSS>(z.y, k.R_rest, true, c2, inv_t)); });
-                if (tid < edges) from_float(out + slice.edge(tid), scale * power_of<LOSS>(to_float(row.base[slice.edge(tid)]), k.R_rest, k.slow, c2, inv_t));
+                else pass([&](float2 z) { return make_float2(power_of(z.x, k.R_rest, true, c2), power_of(z.y, k.R_rest, true, c2)); });
+                if (tid < edges) from_float(out + slice.edge(tid), scale * power_of(to_float(row.base[slice.edge(tid)]), k.R_rest, k.slow, c2));
             }
             __syncthreads();
             if (lister)
                 for (int e = lane; e < slots; e += 32)
-                    if (list_at[e] >= 0) from_float(out + list_at[e], up * fmaf(power_of<LOSS>(list_z[e], k.R, k.slow, c2, inv_t), k.inv, -list_p[e]));
+                    if (list_at[e] >= 0) from_float(out + list_at[e], up * fmaf(power_of(list_z[e], k.R, k.slow, c2), k.inv, -list_p[e]));
         }
     }
     if (LOSS && C > 1) cluster_sync();                    // nobody's shared memory goes while others may still read it
@@ -642,6 +704,7 @@ template <bool LOSS, bool GRAD> cudaError_t launch(const DistillArgs& a, int dty
     plan.inv_t_low = (float)(plan.inv_t_d - (double)plan.inv_t);
     plan.c2 = (float)(kLog2eD / a.temperature);
     plan.kappa = kLog2eD / a.temperature / (double)plan.c2;
+    plan.unit = (double)plan.c2 * a.temperature;
     // Several blocks to a row where the rows alone do not fill the device (a row of 131072 bf16 logits: 14 us on one block, 11.4 us on
     // eight), and where a row is longer than 256 KB
     plan.cluster = 1;
