@@ -100,6 +100,19 @@ def _dtype_code(t) -> int:
     raise TmError(5, "W must be float32 or bfloat16")
 
 
+def _under(stream, fn, args):
+    """fn(**args) with `stream` as torch's current stream, so that the tensors which the call creates (and, for a workspace, drops again)
+    belong to the stream that works on them: the allocator neither gives their memory to another stream nor takes it from one."""
+    import torch
+    args = dict(args, stream=None)
+    first = next(iter(args.values()))
+    device = (first if torch.is_tensor(first) else first[0]).device
+    if stream.device != device:
+        raise TmError(2, "stream must be on the tensors' device")
+    with torch.cuda.stream(stream):
+        return fn(**args)
+
+
 def _outputs(W, mask_out, masked_w_out, objective_out, want_masked, want_objective):
     import torch
     rows, cols = W.shape
@@ -264,6 +277,8 @@ def tm_find_mask_batched(Ws: Sequence, N: int, M: int, method: int, masks=None, 
     `stream` (a torch.cuda.Stream) or on torch's current stream.  With more than one matrix the descriptor tables
     are copied from host memory first (the runtime may wait for the stream's earlier work to do so), and such a
     call is refused on a capturing stream: capture tm_plan_run() instead."""
+    if stream is not None and len(Ws) > 0:
+        return _under(stream, tm_find_mask_batched, locals())
     import torch
     lib = load_library()
     if len(Ws) == 0:
@@ -319,6 +334,8 @@ def tm_nm_mask_1d(W, N: int, M: int, absorb_mean: bool = False, mask_out=None, m
                   violations_out=None, status=None, workspace=None, stream=None, want_masked: bool = True):
     """1-D N:M magnitude pruning along rows (N kept per group of M).  Returns (mask, masked, objective[1],
     violations int64[1], status int32[1]); asynchronous on `stream` or torch's current stream."""
+    if stream is not None:
+        return _under(stream, tm_nm_mask_1d, locals())
     import torch
     lib = load_library()
     if not (W.is_cuda and W.dim() == 2 and (W.shape[1] <= 1 or W.stride(1) == 1)):
@@ -344,6 +361,8 @@ def tm_nm_mask_1d(W, N: int, M: int, absorb_mean: bool = False, mask_out=None, m
 
 def tm_mask_violations(W, mask, violations_out=None, workspace=None, stream=None):
     """Non-zero weights whose bit in the packed mask is 0.  Returns int64[1] (device)."""
+    if stream is not None:
+        return _under(stream, tm_mask_violations, locals())
     import torch
     lib = load_library()
     dev = W.device
@@ -358,6 +377,8 @@ def tm_mask_violations(W, mask, violations_out=None, workspace=None, stream=None
 
 def tm_mask_hamming(mask_a, mask_b, distance_out=None, workspace=None, stream=None):
     """Number of differing bits of two packed masks (same shape).  Returns int64[1] (device)."""
+    if stream is not None:
+        return _under(stream, tm_mask_hamming, locals())
     import torch
     lib = load_library()
     dev = mask_a.device
@@ -375,6 +396,8 @@ def tm_mask_hamming(mask_a, mask_b, distance_out=None, workspace=None, stream=No
 def tm_compress_2_4(W, mask, values=None, meta=None, values_t=None, meta_t=None, status=None, stream=None):
     """2:4 compressed operands of W and W^T from one transposable mask.  Returns (values [rows, cols/2],
     meta int32 [rows, wpr(cols)], values_t [cols, rows/2], meta_t int32 [cols, wpr(rows)], status int32[1])."""
+    if stream is not None:
+        return _under(stream, tm_compress_2_4, locals())
     import torch
     lib = load_library()
     dev = W.device

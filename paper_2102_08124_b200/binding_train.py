@@ -3,7 +3,8 @@ largest logits, and the distillation loss against such lists.  Same names as inc
 marshalling only.
 
 Matrices are 2-D CUDA tensors, float32 or bfloat16, with unit column stride; rows may be strided.  Every call is asynchronous on
-`stream` (a torch.cuda.Stream) or torch's current stream, and creates whichever outputs were not passed in."""
+`stream` (a torch.cuda.Stream) or torch's current stream, and creates whichever outputs were not passed in (on that stream: another one
+that uses them has to wait for it)."""
 from __future__ import annotations
 
 import ctypes
@@ -43,10 +44,10 @@ def _lib():
     return _ready
 
 
-def _call(fn, device, stream, *args):
-    """fn(*args, stream) with `device` current."""
+def _call(fn, device, *args):
+    """fn(*args, torch's current stream) with `device` current."""
     index = device.index
-    s = stream.cuda_stream if stream is not None else _raw_stream(index)
+    s = _raw_stream(index)
     if _torch.cuda.current_device() == index:
         rc = fn(*args, s)
     else:
@@ -112,6 +113,8 @@ def _ptr(t):
 def tm_layer_norm(x, weight=None, bias=None, eps: float = 1e-5, residual=None, y=None, sum_out=None, mean_out=None, rstd_out=None,
                   want_sum: bool = True, want_stats: bool = True, stream=None):
     """Layer norm of x, or of x + residual, over the columns.  Returns (y, x + residual or None, mean, rstd)."""
+    if stream is not None:
+        return binding._under(stream, tm_layer_norm, locals())
     lib = _lib()
     code, dev, rows, cols, ld = _input(x, "x")
     _, wcode, wp, bp = _params(weight, bias, cols, dev, x.dtype)
@@ -138,7 +141,7 @@ def tm_layer_norm(x, weight=None, bias=None, eps: float = 1e-5, residual=None, y
             mean_out = _torch.empty((rows,), dtype=f32, device=dev) if mean_out is None else mean_out
             rstd_out = _torch.empty((rows,), dtype=f32, device=dev) if rstd_out is None else rstd_out
         mp, rp = _array(mean_out, (rows,), f32, dev, "mean_out"), _array(rstd_out, (rows,), f32, dev, "rstd_out")
-    _call(lib.tm_layer_norm, dev, stream, x.data_ptr(), ld, _ptr(residual), ld_r, code, rows, cols, wp, bp, wcode, eps, _ptr(sum_out), ld_s,
+    _call(lib.tm_layer_norm, dev, x.data_ptr(), ld, _ptr(residual), ld_r, code, rows, cols, wp, bp, wcode, eps, _ptr(sum_out), ld_s,
           y.data_ptr(), ld_y, mp, rp)
     return y, sum_out, mean_out, rstd_out
 
@@ -151,6 +154,8 @@ def tm_layer_norm_backward(dy, h, mean, rstd, weight=None, dsum=None, dx=None, d
                            want_params: bool = True, params_dtype=None, stream=None):
     """Gradients of the layer norm of h (x, or the sum that tm_layer_norm returned).  Returns (dx, dweight, dbias); the last two have
     the weight's dtype (without a weight `params_dtype`, or h's), and are None with want_params=False."""
+    if stream is not None:
+        return binding._under(stream, tm_layer_norm_backward, locals())
     lib = _lib()
     code, dev, rows, cols, ld_h = _input(h, "h")
     kind, wcode, wp, _ = _params(weight, None, cols, dev, params_dtype or h.dtype)
@@ -177,7 +182,7 @@ def tm_layer_norm_backward(dy, h, mean, rstd, weight=None, dsum=None, dx=None, d
         else:
             bytes_ = workspace.numel() * workspace.element_size()
         wsp = workspace.data_ptr()
-    _call(lib.tm_layer_norm_backward, dev, stream, dy.data_ptr(), ld_dy, h.data_ptr(), ld_h, code, rows, cols, wp, wcode,
+    _call(lib.tm_layer_norm_backward, dev, dy.data_ptr(), ld_dy, h.data_ptr(), ld_h, code, rows, cols, wp, wcode,
           _array(mean, (rows,), f32, dev, "mean"), _array(rstd, (rows,), f32, dev, "rstd"), _ptr(dsum), ld_s, dx.data_ptr(), ld_dx, dwp, dbp, wsp, bytes_)
     return dx, dweight_out, dbias_out
 
@@ -186,6 +191,8 @@ def tm_top_logits(logits, k: int, temperature: float = 1.0, values_out=None, ids
                   status=None, stream=None):
     """The k largest logits of every row (equal ones by the lower id) and log sum exp(logits / temperature).
     Returns (values float32 [rows, k], ids int32 [rows, k], lse float32 [rows] or None).  status: int32[1] or None."""
+    if stream is not None:
+        return binding._under(stream, tm_top_logits, locals())
     lib = _lib()
     code, dev, rows, vocab, ld = _input(logits, "logits")
     f32, i32, shape = _torch.float32, _torch.int32, (rows, max(k, 0))
@@ -195,7 +202,7 @@ def tm_top_logits(logits, k: int, temperature: float = 1.0, values_out=None, ids
         ids_out = _torch.empty(shape, dtype=i32, device=dev)
     if lse_out is None and want_lse:
         lse_out = _torch.empty((rows,), dtype=f32, device=dev)
-    _call(lib.tm_top_logits, dev, stream, logits.data_ptr(), code, rows, vocab, ld, k, temperature, _array(values_out, shape, f32, dev, "values_out"),
+    _call(lib.tm_top_logits, dev, logits.data_ptr(), code, rows, vocab, ld, k, temperature, _array(values_out, shape, f32, dev, "values_out"),
           _array(ids_out, shape, i32, dev, "ids_out"), _array(lse_out, (rows,), f32, dev, "lse_out"), _array(status, (1,), i32, dev, "status"))
     return values_out, ids_out, lse_out
 
@@ -213,6 +220,8 @@ def _lists(logits, top_values, top_ids, teacher_lse, row_weight, temperature, sc
 def tm_distill_loss(logits, top_values, top_ids, teacher_lse=None, row_weight=None, temperature: float = 1.0, scale: float = 1.0,
                     loss_out=None, stats_out=None, want_stats: bool = True, status=None, stream=None):
     """Loss of every row (float32 [rows]) and the statistics [rows, 2] that tm_distill_grad takes."""
+    if stream is not None:
+        return binding._under(stream, tm_distill_loss, locals())
     lib = _lib()
     dev, rows, head = _lists(logits, top_values, top_ids, teacher_lse, row_weight, temperature, scale)
     f32 = _torch.float32
@@ -220,7 +229,7 @@ def tm_distill_loss(logits, top_values, top_ids, teacher_lse=None, row_weight=No
         loss_out = _torch.empty((rows,), dtype=f32, device=dev)
     if stats_out is None and want_stats:
         stats_out = _torch.empty((rows, 2), dtype=f32, device=dev)
-    _call(lib.tm_distill_loss, dev, stream, *head, _array(loss_out, (rows,), f32, dev, "loss_out"),
+    _call(lib.tm_distill_loss, dev, *head, _array(loss_out, (rows,), f32, dev, "loss_out"),
           _array(stats_out, (rows, 2), f32, dev, "stats_out"), _array(status, (1,), _torch.int32, dev, "status"))
     return loss_out, stats_out
 
@@ -228,6 +237,8 @@ def tm_distill_loss(logits, top_values, top_ids, teacher_lse=None, row_weight=No
 def tm_distill_grad(logits, top_values, top_ids, stats, grad_loss=None, teacher_lse=None, row_weight=None, temperature: float = 1.0,
                     scale: float = 1.0, dlogits=None, status=None, stream=None):
     """Gradient of the logits from the statistics of tm_distill_loss, times grad_loss[row] where given."""
+    if stream is not None:
+        return binding._under(stream, tm_distill_grad, locals())
     lib = _lib()
     dev, rows, head = _lists(logits, top_values, top_ids, teacher_lse, row_weight, temperature, scale)
     f32, ld_d = _torch.float32, logits.shape[1]
@@ -235,7 +246,7 @@ def tm_distill_grad(logits, top_values, top_ids, stats, grad_loss=None, teacher_
         ld_d = _other(dlogits, "dlogits", logits)
     else:
         dlogits = _like(logits)
-    _call(lib.tm_distill_grad, dev, stream, *head, _array(stats, (rows, 2), f32, dev, "stats"), _array(grad_loss, (rows,), f32, dev, "grad_loss"),
+    _call(lib.tm_distill_grad, dev, *head, _array(stats, (rows, 2), f32, dev, "stats"), _array(grad_loss, (rows,), f32, dev, "grad_loss"),
           dlogits.data_ptr(), ld_d, _array(status, (1,), _torch.int32, dev, "status"))
     return dlogits
 
@@ -243,6 +254,8 @@ def tm_distill_grad(logits, top_values, top_ids, stats, grad_loss=None, teacher_
 def tm_distill_loss_grad(logits, top_values, top_ids, teacher_lse=None, row_weight=None, temperature: float = 1.0, scale: float = 1.0,
                          loss_out=None, dlogits=None, status=None, stream=None):
     """Loss of every row and the gradient of their sum, in one pass over the logits.  Returns (loss [rows], dlogits)."""
+    if stream is not None:
+        return binding._under(stream, tm_distill_loss_grad, locals())
     lib = _lib()
     dev, rows, head = _lists(logits, top_values, top_ids, teacher_lse, row_weight, temperature, scale)
     ld_d = logits.shape[1]
@@ -252,6 +265,6 @@ def tm_distill_loss_grad(logits, top_values, top_ids, teacher_lse=None, row_weig
         ld_d = _other(dlogits, "dlogits", logits)
     else:
         dlogits = _like(logits)
-    _call(lib.tm_distill_loss_grad, dev, stream, *head, _array(loss_out, (rows,), _torch.float32, dev, "loss_out"), dlogits.data_ptr(), ld_d,
+    _call(lib.tm_distill_loss_grad, dev, *head, _array(loss_out, (rows,), _torch.float32, dev, "loss_out"), dlogits.data_ptr(), ld_d,
           _array(status, (1,), _torch.int32, dev, "status"))
     return loss_out, dlogits
