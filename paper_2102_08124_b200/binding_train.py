@@ -180,6 +180,8 @@ def tm_layer_norm_backward(dy, h, mean, rstd, weight=None, dsum=None, dx=None, d
             bytes_ = lib.tm_layer_norm_workspace_bytes(rows, cols)
             workspace = _torch.empty((bytes_,), dtype=_torch.uint8, device=dev)
         else:
+            if workspace.device != dev or not workspace.is_contiguous():
+                raise TmError(8, "workspace must be a contiguous tensor on the matrix's device")
             bytes_ = workspace.numel() * workspace.element_size()
         wsp = workspace.data_ptr()
     _call(lib.tm_layer_norm_backward, dev, dy.data_ptr(), ld_dy, h.data_ptr(), ld_h, code, rows, cols, wp, wcode,
