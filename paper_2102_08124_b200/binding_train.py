@@ -112,21 +112,20 @@ def _ptr(t):
 
 def tm_layer_norm(x, weight=None, bias=None, eps: float = 1e-5, residual=None, y=None, sum_out=None, mean_out=None, rstd_out=None,
                   want_sum: bool = True, want_stats: bool = True, stream=None):
-    """Layer norm of x, or of x + residual, over the columns.  Returns (y, x + residual or None, mean, rstd)."""
+    """Layer norm of x, or of x + residual, over the columns.  Returns (y, the sum, mean, rstd); the sum is None without a residual,
+    unless sum_out was passed in (it receives x then)."""
     if stream is not None:
         return binding._under(stream, tm_layer_norm, locals())
     lib = _lib()
     code, dev, rows, cols, ld = _input(x, "x")
     _, wcode, wp, bp = _params(weight, bias, cols, dev, x.dtype)
     ld_r = ld_s = ld_y = cols
-    if residual is None:
-        sum_out = None
-    else:
+    if residual is not None:
         ld_r = _other(residual, "residual", x)
-        if sum_out is not None:
-            ld_s = _other(sum_out, "sum_out", x)
-        elif want_sum:
+        if sum_out is None and want_sum:
             sum_out = _like(x)
+    if sum_out is not None:
+        ld_s = _other(sum_out, "sum_out", x)
     if y is not None:
         ld_y = _other(y, "y", x)
     else:

@@ -16,3 +16,12 @@ def test_a_workspace_that_the_gpu_cannot_use_is_refused():
         with pytest.raises(tm.TmError):
             tm.tm_layer_norm_backward(x, x, stat, stat, workspace=workspace)
     tm.tm_layer_norm_backward(x, x, stat, stat, workspace=torch.empty(n, dtype=torch.uint8, device="cuda"))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("cols", [40, 1001, 9000, 20000])
+def test_a_sum_that_was_passed_in_is_written_without_a_residual(cols, dtype):
+    x = torch.randn(7, cols, device="cuda").to(dtype)
+    out = torch.full_like(x, float("nan"))
+    y, s, _, _ = tm.tm_layer_norm(x, sum_out=out)
+    assert s is out and torch.equal(out, x) and torch.equal(y, tm.tm_layer_norm(x)[0]) and tm.tm_layer_norm(x)[1] is None
