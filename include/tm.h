@@ -281,7 +281,8 @@ int tm_layer_norm_backward(const void* dy, int64_t ld_dy, const void* h, int64_t
                            void* dx, int64_t ld_dx, void* dweight_out, void* dbias_out, void* workspace_dev, size_t workspace_bytes, void* cuda_stream);
 
 /*
- * tm_top_logits -- the k largest logits of every row, largest first, equal ones by the lower id (1 <= k <= TM_TOP_MAX):
+ * tm_top_logits -- the k largest logits of every row, largest first, equal ones by the lower id (1 <= k <= TM_TOP_MAX; the temperature
+ * is finite and a positive number of fp32's normal range, here and below):
  * values_out[rows][k] (fp32, not divided by the temperature), ids_out[rows][k]; where k > vocab the list ends in (-Inf, -1).
  * -0 counts as 0, NaN is larger than everything.  lse_out (rows floats, may be NULL): log sum_j exp(logit_j / temperature) over the
  * whole row.  -Inf (a masked logit) is an ordinary value; NaN and +Inf raise TM_DEV_NONFINITE in *status_dev (may be NULL).

@@ -1,4 +1,5 @@
 // C ABI of the operators of the training step around the masked layers (see include/tm.h): argument checks and dispatch.
+#include <cfloat>
 #include <cmath>
 
 #include "../../include/tm.h"
@@ -15,6 +16,9 @@ bool good_rows(int64_t rows, int64_t cols) { return rows >= 0 && cols >= 0; }
 // a matrix's leading dimension: rows must not overlap, and offsets must stay inside 63 bits
 bool good_ld(int64_t rows, int64_t cols, int64_t ld) { return ld >= cols && (rows == 0 || ld <= (INT64_MAX / 8) / rows); }
 
+// logits are scaled by log2(e) / T: below the normal range that has no fp32 value
+bool good_temperature(float t) { return t >= FLT_MIN && std::isfinite(t); }
+
 int finish(cudaError_t e) {
     if (e == cudaSuccess) return TM_OK;
     cudaGetLastError();
@@ -28,7 +32,7 @@ struct Lists {
 int check_distill(const void* logits, int dtype, int64_t rows, int64_t vocab, int64_t ld, const Lists& l, const int* status) {
     if (!good_dtype(dtype)) return TM_ERR_DTYPE;
     if (!good_rows(rows, vocab) || !good_ld(rows, vocab, ld) || vocab > TM_VOCAB_MAX) return TM_ERR_SHAPE;
-    if (l.k < 0 || l.k > TM_TOP_MAX || !(l.temperature > 0.0f) || !std::isfinite(l.temperature) || !std::isfinite(l.scale)) return TM_ERR_RANGE;
+    if (l.k < 0 || l.k > TM_TOP_MAX || !good_temperature(l.temperature) || !std::isfinite(l.scale)) return TM_ERR_RANGE;
     if (rows == 0) return TM_OK;
     if ((vocab > 0 && !logits) || (l.k > 0 && (!l.values || !l.ids))) return TM_ERR_NULL;
     if (off(logits, elem_bytes(dtype)) || off(l.values, 4) || off(l.ids, 4) || off(l.teacher_lse, 4) || off(l.row_weight, 4) || off(status, 4)) return TM_ERR_ALIGN;
@@ -106,7 +110,7 @@ int tm_top_logits(const void* logits, int dtype, int64_t rows, int64_t vocab, in
                   float* values_out, int32_t* ids_out, float* lse_out, int* status_dev, void* cuda_stream) {
     if (!good_dtype(dtype)) return TM_ERR_DTYPE;
     if (!good_rows(rows, vocab) || !good_ld(rows, vocab, ld) || vocab > TM_VOCAB_MAX) return TM_ERR_SHAPE;
-    if (k < 1 || k > TM_TOP_MAX || !(temperature > 0.0f) || !std::isfinite(temperature)) return TM_ERR_RANGE;
+    if (k < 1 || k > TM_TOP_MAX || !good_temperature(temperature)) return TM_ERR_RANGE;
     if (rows == 0) return TM_OK;
     if ((vocab > 0 && !logits) || !values_out || !ids_out) return TM_ERR_NULL;
     if (off(logits, elem_bytes(dtype)) || off(values_out, 4) || off(ids_out, 4) || off(lse_out, 4) || off(status_dev, 4)) return TM_ERR_ALIGN;
