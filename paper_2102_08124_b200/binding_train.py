@@ -196,7 +196,9 @@ def tm_top_logits(logits, k: int, temperature: float = 1.0, values_out=None, ids
         return binding._under(stream, tm_top_logits, locals())
     lib = _lib()
     code, dev, rows, vocab, ld = _input(logits, "logits")
-    f32, i32, shape = _torch.float32, _torch.int32, (rows, max(k, 0))
+    if not 1 <= k <= TM_TOP_MAX:                            # before anything of that size is created
+        raise TmError(TM_ERR_RANGE, binding.tm_status_string(TM_ERR_RANGE))
+    f32, i32, shape = _torch.float32, _torch.int32, (rows, k)
     if values_out is None:
         values_out = _torch.empty(shape, dtype=f32, device=dev)
     if ids_out is None:

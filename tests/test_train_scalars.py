@@ -14,6 +14,16 @@ def test_temperatures_below_the_normal_range_are_refused(lib, t):  # noqa: F811
     assert all(_distill(lib, which, t=t) == tm.TM_ERR_RANGE for which in ("loss", "grad", "both"))
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("k", [-1, 0, 257, 10 ** 12, 2 ** 32 + 1])
+def test_list_lengths_are_refused_before_anything_is_created(k):
+    import torch
+    z = torch.zeros(4, 300, device="cuda")
+    with pytest.raises(tm.TmError) as e:
+        tm.tm_top_logits(z, k)
+    assert e.value.code == tm.TM_ERR_RANGE
+
+
 def _rounded(x):
     """As fp32 has it: infinite past its range."""
     with np.errstate(over="ignore"):
