@@ -39,6 +39,7 @@ def _rows(t):
 
 def _make():
     import torch
+    from torch.autograd.function import once_differentiable              # second derivatives are refused, not left out
 
     class Norm(torch.autograd.Function):
         @staticmethod
@@ -53,6 +54,7 @@ def _make():
             return y.view(x.shape), None if residual is None else h.view(x.shape)
 
         @staticmethod
+        @once_differentiable
         def backward(ctx, dy, dsum):
             h, mean, rstd, weight = ctx.saved_tensors
             want = ctx.params[0] and any(ctx.needs_input_grad[2:4])
@@ -74,6 +76,7 @@ def _make():
             return loss
 
         @staticmethod
+        @once_differentiable
         def backward(ctx, grad):
             z, values, ids, lse, row_weight, stats = ctx.saved_tensors
             temperature, scale, shape = ctx.scalars

@@ -1,0 +1,33 @@
+"""The autograd forms of the training operators: second derivatives, gradients in both types, shapes."""
+from __future__ import annotations
+
+import pytest
+import torch
+
+from paper_2102_08124_b200.distill import distill_backward, distill_loss, layer_norm, teacher_lists
+from tests import train_ref as ref
+
+pytestmark = pytest.mark.gpu
+
+
+def test_a_second_differentiation_is_refused():
+    """A gradient penalty through these operators would lose terms: it raises instead."""
+    x, r, w = (torch.randn(*s, device="cuda", requires_grad=True) for s in ((5, 16), (5, 16), (16,)))
+    y, h = layer_norm(x, w, residual=r)
+    (g,) = torch.autograd.grad((y.square() + h).sum(), x, create_graph=True)
+    with pytest.raises(RuntimeError):
+        g.square().sum().backward()
+    z = torch.randn(4, 50, device="cuda", requires_grad=True)
+    lists = teacher_lists(torch.randn(4, 50, device="cuda"), 5)
+    (g,) = torch.autograd.grad(distill_loss(z, lists).sum(), z, create_graph=True)
+    with pytest.raises(RuntimeError):
+        g.square().sum().backward()
+
+
+def test_one_differentiation_with_a_graph_kept():
+    x = torch.randn(5, 16, device="cuda", requires_grad=True)
+    y, _ = layer_norm(x)
+    c = torch.randn_like(y)
+    first = torch.autograd.grad((y * c).sum(), x, create_graph=True)[0]
+    second = torch.autograd.grad((y * c).sum(), x)[0]
+    assert torch.equal(first, second)
