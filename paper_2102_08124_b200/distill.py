@@ -44,6 +44,8 @@ def _make():
     class Norm(torch.autograd.Function):
         @staticmethod
         def forward(ctx, x, residual, weight, bias, eps):
+            if residual is not None and residual.shape != x.shape:       # rows of other shapes could still be as many
+                raise tm.TmError(2, "residual must have the shape of x")
             x2 = _rows(x)
             y, h, mean, rstd = tt.tm_layer_norm(x2, weight, bias, eps, residual=None if residual is None else _rows(residual))
             h = x2 if residual is None else h

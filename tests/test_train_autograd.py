@@ -31,3 +31,12 @@ def test_one_differentiation_with_a_graph_kept():
     first = torch.autograd.grad((y * c).sum(), x, create_graph=True)[0]
     second = torch.autograd.grad((y * c).sum(), x)[0]
     assert torch.equal(first, second)
+
+
+def test_a_residual_of_another_shape_is_refused():
+    """(2, 3, n) and (3, 2, n) have as many rows, but not the same ones."""
+    from paper_2102_08124_b200 import TmError
+    x = torch.randn(2, 3, 16, device="cuda")
+    for other in (x.transpose(0, 1), x.reshape(6, 16), x[:1], x[..., :8]):
+        with pytest.raises(TmError):
+            layer_norm(x, residual=other)
