@@ -71,6 +71,8 @@ def _make():
     class Loss(torch.autograd.Function):
         @staticmethod
         def forward(ctx, logits, values, ids, lse, row_weight, temperature, scale):
+            if any(ctx.needs_input_grad[1:]):
+                raise tm.TmError(2, "the loss has a gradient for its logits alone: detach the teacher's lists and the row weights")
             z = _rows(logits)
             loss, stats = tt.tm_distill_loss(z, values, ids, lse, row_weight, temperature, scale, want_stats=ctx.needs_input_grad[0])
             ctx.save_for_backward(z, values, ids, lse, row_weight, stats)

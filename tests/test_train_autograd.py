@@ -40,3 +40,19 @@ def test_a_residual_of_another_shape_is_refused():
     for other in (x.transpose(0, 1), x.reshape(6, 16), x[:1], x[..., :8]):
         with pytest.raises(TmError):
             layer_norm(x, residual=other)
+
+
+def test_a_gradient_that_the_loss_does_not_have_is_refused():
+    from paper_2102_08124_b200 import TmError
+    z = torch.randn(4, 50, device="cuda", requires_grad=True)
+    lists = teacher_lists(torch.randn(4, 50, device="cuda"), 5)
+    weight = torch.ones(4, device="cuda", requires_grad=True)
+    with pytest.raises(TmError):
+        distill_loss(z, lists, weight)
+    with pytest.raises(TmError):
+        distill_loss(z, lists._replace(values=lists.values.clone().requires_grad_()))
+    with pytest.raises(TmError):
+        distill_loss(z, lists._replace(lse=lists.lse.clone().requires_grad_()))
+    distill_loss(z, lists, weight.detach()).sum().backward()
+    with torch.no_grad():
+        distill_loss(z, lists, weight)
