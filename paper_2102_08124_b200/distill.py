@@ -71,8 +71,6 @@ def _make():
     class Loss(torch.autograd.Function):
         @staticmethod
         def forward(ctx, logits, values, ids, lse, row_weight, temperature, scale):
-            if any(ctx.needs_input_grad[1:]):
-                raise tm.TmError(2, "the loss has a gradient for its logits alone: detach the teacher's lists and the row weights")
             z = _rows(logits)
             loss, stats = tt.tm_distill_loss(z, values, ids, lse, row_weight, temperature, scale, want_stats=ctx.needs_input_grad[0])
             ctx.save_for_backward(z, values, ids, lse, row_weight, stats)
@@ -105,6 +103,9 @@ def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, residual=None):
 
 def distill_loss(logits, teacher: TeacherLists, row_weight=None, scale: float = 1.0):
     """Differentiable loss of every row of logits [..., vocab] (float32 [rows])."""
+    import torch
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (teacher.values, teacher.lse, row_weight)):
+        raise tm.TmError(2, "the loss has a gradient for its logits alone: detach the teacher's lists and the row weights")
     return _get()[1].apply(logits, teacher.values, teacher.ids, teacher.lse, row_weight, teacher.temperature, scale)
 
 
