@@ -70,9 +70,9 @@ def _make():
 
     class Loss(torch.autograd.Function):
         @staticmethod
-        def forward(ctx, logits, values, ids, lse, row_weight, temperature, scale):
+        def forward(ctx, logits, values, ids, lse, row_weight, temperature, scale, status):
             z = _rows(logits)
-            loss, stats = tt.tm_distill_loss(z, values, ids, lse, row_weight, temperature, scale, want_stats=ctx.needs_input_grad[0])
+            loss, stats = tt.tm_distill_loss(z, values, ids, lse, row_weight, temperature, scale, want_stats=ctx.needs_input_grad[0], status=status)
             ctx.save_for_backward(z, values, ids, lse, row_weight, stats)
             ctx.scalars = (temperature, scale, logits.shape)
             return loss
@@ -83,7 +83,7 @@ def _make():
             z, values, ids, lse, row_weight, stats = ctx.saved_tensors
             temperature, scale, shape = ctx.scalars
             d = tt.tm_distill_grad(z, values, ids, stats, grad.contiguous(), lse, row_weight, temperature, scale)
-            return d.view(shape), None, None, None, None, None, None
+            return (d.view(shape),) + (None,) * 7
 
     return Norm, Loss
 
@@ -101,18 +101,18 @@ def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, residual=None):
     return y, x if residual is None else h
 
 
-def distill_loss(logits, teacher: TeacherLists, row_weight=None, scale: float = 1.0):
-    """Differentiable loss of every row of logits [..., vocab] (float32 [rows])."""
+def distill_loss(logits, teacher: TeacherLists, row_weight=None, scale: float = 1.0, status=None):
+    """Differentiable loss of every row of logits [..., vocab] (float32 [rows]).  status (int32[1] or None): TM_DEV_BADID for ids that were left out."""
     import torch
     if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (teacher.values, teacher.lse, row_weight)):
         raise tm.TmError(2, "the loss has a gradient for its logits alone: detach the teacher's lists and the row weights")
-    return _get()[1].apply(logits, teacher.values, teacher.ids, teacher.lse, row_weight, teacher.temperature, scale)
+    return _get()[1].apply(logits, teacher.values, teacher.ids, teacher.lse, row_weight, teacher.temperature, scale, status)
 
 
-def distill_backward(logits, teacher: TeacherLists, row_weight=None, scale: float = 1.0):
+def distill_backward(logits, teacher: TeacherLists, row_weight=None, scale: float = 1.0, status=None):
     """Adds the gradient of the summed loss to everything that logits [..., vocab] came from, and returns the loss of every row: loss and
     gradient in one pass over the logits, for a step that has no other use of the loss."""
-    loss, d = tt.tm_distill_loss_grad(_rows(logits.detach()), teacher.values, teacher.ids, teacher.lse, row_weight, teacher.temperature, scale)
+    loss, d = tt.tm_distill_loss_grad(_rows(logits.detach()), teacher.values, teacher.ids, teacher.lse, row_weight, teacher.temperature, scale, status=status)
     logits.backward(d.view(logits.shape))
     return loss
 

@@ -56,3 +56,17 @@ def test_a_gradient_that_the_loss_does_not_have_is_refused():
     distill_loss(z, lists, weight.detach()).sum().backward()
     with torch.no_grad():
         distill_loss(z, lists, weight)
+
+
+def test_ids_that_were_left_out_are_seen():
+    import paper_2102_08124_b200 as tm
+    z = torch.randn(4, 50, device="cuda", requires_grad=True)
+    lists = teacher_lists(torch.randn(4, 50, device="cuda"), 5)
+    bad = lists._replace(ids=lists.ids.clone())
+    bad.ids[2, 1] = 50
+    for call in (lambda l, s: distill_loss(z, l, status=s), lambda l, s: distill_backward(z * 1, l, status=s)):
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        call(lists, status)
+        assert int(status) == 0
+        call(bad, status)
+        assert int(status) == tm.TM_DEV_BADID
