@@ -70,3 +70,59 @@ def test_ids_that_were_left_out_are_seen():
         assert int(status) == 0
         call(bad, status)
         assert int(status) == tm.TM_DEV_BADID
+
+
+def _norm64(x, r, w, b):
+    h = x + r
+    m = h.mean(-1, keepdim=True)
+    return (h - m) / ((h - m).square().mean(-1, keepdim=True) + 1e-5).sqrt() * w + b, h
+
+
+@pytest.mark.parametrize("shape", [(3, 11, 200), (40, 1024), (2, 9000)])
+def test_layer_norm_gradients_in_bf16(shape):
+    """Against 64-bit autograd: the stored sum, y's gradient and the result are rounded to bf16 once each (2^-9 of an entry, or of the largest
+    one where it enters all of a row); the sums over n rows add theirs like n^(1/2)."""
+    torch.manual_seed(6)
+    n = shape[-1]
+    leaf = lambda *s: torch.randn(*s, device="cuda").bfloat16().requires_grad_()
+    x, r, w, b = leaf(*shape), leaf(*shape), leaf(n), leaf(n)
+    c, e = (torch.randn(*shape, device="cuda").bfloat16() for _ in range(2))
+    y, h = layer_norm(x, w, b, residual=r)
+    torch.autograd.backward([y, h], [c, e])
+    X, R, W, B = (t.detach().double().requires_grad_() for t in (x, r, w, b))
+    Y, H = _norm64(X, R, W, B)
+    torch.autograd.backward([Y, H], [c.double(), e.double()])
+    close = lambda got, want, unit: float((got.double() - want).abs().max()) <= unit * float(want.abs().max())
+    assert close(y.detach(), Y.detach(), 2.0 ** -8) and close(h.detach(), H.detach(), 2.0 ** -8)
+    assert close(x.grad, X.grad, 2.0 ** -6) and close(r.grad, R.grad, 2.0 ** -6)
+    assert close(w.grad, W.grad, 2.0 ** -6) and close(b.grad, B.grad, 2.0 ** -7)
+
+
+@pytest.mark.parametrize("tail", [False, True])
+def test_distill_gradients_in_bf16(tail):
+    """Against 64-bit autograd: every entry of the gradient is rounded to bf16 once, beside fp32 exponentials."""
+    torch.manual_seed(7)
+    rows, vocab, t, scale = 9, 3001, 1.5, 2.0
+    teacher, z = (3 * torch.randn(3, 3, vocab, device="cuda") for _ in range(2))
+    z = z.bfloat16().requires_grad_()
+    lists = teacher_lists(teacher.reshape(rows, vocab), 20, t)
+    lists = lists if tail else lists._replace(lse=None)
+    up, weight = torch.rand(rows, device="cuda") + 0.5, torch.rand(rows, device="cuda")
+    loss = distill_loss(z, lists, weight, scale)
+    (loss * up).sum().backward()
+    Z = z.detach().double().reshape(rows, vocab).requires_grad_()
+    logq, at = (Z / t).log_softmax(1), lists.ids.long()
+    v = lists.values.double() / t
+    logp = v - lists.lse.double()[:, None] if tail else v.log_softmax(1)
+    want = (logp.exp() * (logp - logq.gather(1, at))).sum(1)
+    if tail:
+        out = torch.ones_like(logq, dtype=torch.bool).scatter_(1, at, False)
+        rest = 1 - logp.exp().sum(1)
+        want = want + rest * (rest.log() - logq.masked_fill(~out, -torch.inf).logsumexp(1))
+    want = want * scale * weight.double()
+    (want * up).sum().backward()
+    reach = float((z.detach().float() / t).abs().max())
+    unit = 4 * ref.sum_unit(vocab, reach)
+    assert bool(((loss - want).abs() <= unit * (2 + reach) * scale).all())
+    size = Z.grad.abs() + (scale / t * up * weight).double()[:, None] * (logq.detach().exp() + torch.zeros_like(logq).scatter_(1, at, logp.exp()))
+    assert bool(((z.grad.reshape(rows, vocab).double() - Z.grad).abs() <= 2.0 ** -8 * Z.grad.abs() + 2 * unit * size).all())
