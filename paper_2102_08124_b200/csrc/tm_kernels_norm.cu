@@ -465,10 +465,9 @@ __global__ void __launch_bounds__(kRingThreads, 1) ring_norm_backward_kernel(con
     float next_mean = 0.0f, next_rstd = 0.0f;
     if (first < a.rows) { next_mean = a.mean[first]; next_rstd = a.rstd[first]; }
     for (long long r = first; r < a.rows; r += step, turn ^= 1) {
-        float mean = next_mean;
-        const float rstd = next_rstd;
+        const float mean = next_mean, rstd = next_rstd;
         if (r + step < a.rows) { next_mean = a.mean[r + step]; next_rstd = a.rstd[r + step]; }
-        if (!mbar_wait_bounded(ring.bars + slot, phase)) mean = __uint_as_float(0x7FC00000u);     // a row whose copy did not come in time shows as NaN
+        const bool late = !mbar_wait_bounded(ring.bars + slot, phase);
         const RowInStage<DT, VB> dy(plan.in[0], r, plan.row_bytes, ring.stage(slot, 0)), h(plan.in[1], r, plan.row_bytes, ring.stage(slot, 1));
         float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
@@ -513,7 +512,18 @@ __global__ void __launch_bounds__(kRingThreads, 1) ring_norm_backward_kernel(con
                 A::store(dxr + c, o);
             }
         }
-        row_barrier<TPR>();
+        if (__syncthreads_or(late)) {
+            // A copy that did not come in time: this block asks for no more and shows it, in this row, its later ones and its share of the
+            // parameters' gradients.  What is still under way gets some more time before the stages go.
+            const float nan = __uint_as_float(0x7FC00000u);
+            if (t == 0)
+                for (int i = 0; i < plan.stages; ++i) { mbar_wait_bounded(bars + i, 0, 1u << 14); mbar_wait_bounded(bars + i, 1, 1u << 14); }
+            for (; r < a.rows; r += step)
+                for (int c = t; c < cols; c += TPR) from_float(row_of<DT>(a.dx, a.ld_dx, r) + c, nan);
+#pragma unroll
+            for (int k = 0; k < E; ++k) dw[k] = db[k] = nan;
+            break;
+        }
         if (t == 0 && r + plan.stages * step < a.rows) ring.ask(slot, r + plan.stages * step);
         if (++slot == plan.stages) { slot = 0; phase ^= 1u; }
     }
