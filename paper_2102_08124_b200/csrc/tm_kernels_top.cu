@@ -5,7 +5,8 @@
 //
 // Bound: HBM (about six instructions a logit, one of them an exponential).  A thread block goes through its row -- or its slice of
 // one, where a cluster shares a row -- twice.  Pass 1 takes the softmax's running maximum and sum and every thread's largest logit.
-// The k-th largest of those is a bound that at least k logits reach, and few more do (of 131072 random ones and k = 64 some 75).
+// The k-th largest of those is a bound that at least k logits reach, and few more do (of 131072 random ones and k = 64 some 75).  A
+// slice of fewer vectors than k, or a list longer than the block, has none; the buffer then holds the whole slice.
 // Pass 2 collects the logits that reach it: a comparison for a vector.  What shared memory had room for in pass 1 comes from there,
 // the rest from L2, so that HBM is read once.  The entries are then put in order by counting, for each, the larger ones.
 // Where far more reach the bound than the buffer holds (few threads have seen all the large ones), the vectors are gone through
@@ -433,7 +434,12 @@ cudaError_t launch_top(const TopArgs& a, int dtype, int sms, cudaStream_t stream
     plan.slice_vectors = (vectors + plan.cluster - 1) / plan.cluster;
     // Short rows by small blocks, of which more are under way (4096 x 1000 bf16: 25 us with 128 threads, 44 with 256); the longest by
     // large ones, whose rows then fit L2 (4096 x 131072 bf16: 335 us with 256, 333 with 512; 64 x 100000: 17.7 and 14.8)
-    const int nt = vectors > 8192 ? 512 : vectors > 1024 || a.rows <= 2ll * sms ? 256 : 128;
+    // A list longer than the block has no bound (too few threads' maxima) and takes in the whole row: as fast where that fits the buffer
+    // (4096 x 1000 fp32, k 200: 73 us with 128 threads, 89 with 256; x 1700 bf16: 109 and 120), else not (x 4000 fp32, k 129: 151 and
+    // 81; x 8000 bf16, k 200: 294 and 146)
+    static_assert(kCapacity<kF32, 128> == kCapacity<kBF16, 128>, "one limit for both types");
+    const bool longer = a.k > 128 && a.vocab > kCapacity<kF32, 128> - 32;
+    const int nt = vectors > 8192 ? 512 : vectors > 1024 || a.rows <= 2ll * sms || longer ? 256 : 128;
     if (dtype == kF32) return nt == 512 ? launch_rows<kF32, 512>(a, plan, stream) : nt == 128 ? launch_rows<kF32, 128>(a, plan, stream) : launch_rows<kF32, 256>(a, plan, stream);
     return nt == 512 ? launch_rows<kBF16, 512>(a, plan, stream) : nt == 128 ? launch_rows<kBF16, 128>(a, plan, stream) : launch_rows<kBF16, 256>(a, plan, stream);
 }

@@ -1,0 +1,26 @@
+"""Lists as long as they may be, over many short rows."""
+from __future__ import annotations
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2102_08124_b200 as tm
+from tests import train_ref as ref
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("k", [128, 129, 200, 256])
+@pytest.mark.parametrize("rows,vocab", [(1000, 130), (700, 1030), (600, 2311), (500, 4000), (400, 8000)])
+def test_long_lists_of_many_short_rows(rows, vocab, k, dtype):
+    rng = np.random.Generator(np.random.PCG64(k + vocab))
+    z = torch.from_numpy(np.round(rng.standard_normal((rows, vocab)) * 64).astype(np.float32) / 16).to(dtype)      # many equal ones
+    values, ids, lse = (t.double().cpu().numpy() for t in tm.tm_top_logits(z.cuda(), k, 1.5))
+    exact = z.double().numpy()
+    for r in range(0, rows, 7):
+        v, i = ref.top(exact[r], k)
+        assert np.array_equal(ids[r], i) and np.array_equal(values[r], v), r
+    want = np.array([ref.log_sum_exp(x / 1.5) for x in exact])
+    assert np.all(np.abs(lse - want) <= ref.sum_unit(vocab, np.abs(exact).max() / 1.5) + 2 * ref.U32 * np.abs(want))
