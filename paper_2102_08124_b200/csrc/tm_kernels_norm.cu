@@ -657,7 +657,8 @@ template <int DT, int VB, int E> cudaError_t ring_backward(const NormBackArgs& a
 // The form for a row of `cols` elements: threads that share it, elements of each; the fewest threads that keep it in registers, unless
 // measured otherwise (us, the form taken and the other): forward 16384 x 1024 bf16 (128, 8) 23.1, (64, 16) 24.3; 4097 x 1001 fp32 (64, 16)
 // 7.8, (128, 8) 9.1; 16384 x 2048 bf16 (128, 16) 27.8, (256, 8) 29.6; 2048 x 8192 fp32 (1024, 8) 25.6, (512, 16) 29.6; 2047 x 8191 bf16
-// (512, 16) 26.1, (1024, 8) 39.0; wider bf16 (512, 32) 2000 x 16384 51.5 and 200 x 12000 9.2, (1024, 16) 45.2 and 11.3; 3000 x 9000 fp32
+// (512, 16) 26.1, (1024, 8) 39.0; wider bf16 (512, 32) and (1024, 16) by rows times columns: 200 x 12000 7.8 and 9.9, 444 x 16384 14.2 and
+// 15.0, 600 x 12000 17.5 and 17.9, 600 x 16384 22.1 and 19.5, 2000 x 8200 42.4 and 40.3, 2000 x 16384 58.5 and 44.8; 3000 x 9000 fp32
 // (1024, 16) 49.2, (512, 32) 66.0; backward 32768 x 512 bf16
 // (64, 8) 30.1, (128, 8) 46.4; 8000 x 4096 bf16 (256, 16) 53.2, (512, 8) 68.4; 2047 x 8191 bf16 in accesses of one (1024, 8) 63.0,
 // (512, 16) 70.1 (both without kFetch).  Accesses of 16 bytes around such a row's elements, shifted into place, were no faster there
@@ -671,7 +672,9 @@ template <int DT, int VB> cudaError_t forward_by_width(const NormArgs& a, int sm
     if (a.cols <= 4096) return forward<DT, VB, 256, 16>(a, sms, stream);
     constexpr bool kWords = VB == 16 && DT == kF32;
     if (a.cols <= 8192) return forward<DT, VB, kWords ? 1024 : 512, kWords ? 8 : 16>(a, sms, stream);
-    return forward<DT, VB, DT == kBF16 ? 512 : 1024, DT == kBF16 ? 32 : 16>(a, sms, stream);
+    // few wide bf16 rows by fewer threads (a shorter chain for a row), many by more (a row's loads cover another's reductions)
+    if constexpr (DT == kBF16) { if (a.rows * a.cols <= 55000ll * sms) return forward<DT, VB, 512, 32>(a, sms, stream); }
+    return forward<DT, VB, 1024, 16>(a, sms, stream);
 }
 template <int DT, int VB> cudaError_t backward_by_width(const NormBackArgs& a, int sms, int* used, cudaStream_t stream) {
     if (a.cols <= 64) return backward<DT, VB, 8, 8>(a, sms, used, stream);
