@@ -263,7 +263,7 @@ int tm_compress_2_4(const void* W, int dtype, int64_t rows, int64_t cols, int64_
  * tm_layer_norm -- h = x + residual (residual NULL: h = x); over the columns of every row mu = mean(h),
  * rstd = 1 / sqrt(mean((h - mu)^2) + eps), y = (h - mu) * rstd * weight + bias.  weight, bias: cols entries of weight_dtype, NULL
  * for ones and zeros.  sum_out (may be NULL) receives h rounded to dtype, mean_out and rstd_out (rows floats each, may be NULL)
- * the statistics; y comes from h before rounding.  y or sum_out may lie on x or residual.
+ * the statistics; y comes from h before rounding.  y or sum_out may lie on x or residual.  With cols 0 nothing is written.
  *
  * tm_layer_norm_backward -- with g = dy * weight and xh = (h - mean) * rstd:
  *   dx = rstd * (g - mean_c(g) - xh * mean_c(g * xh)) + dsum,   dweight = sum_r(dy * xh),   dbias = sum_r(dy).

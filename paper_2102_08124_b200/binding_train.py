@@ -142,6 +142,10 @@ def tm_layer_norm(x, weight=None, bias=None, eps: float = 1e-5, residual=None, y
         mp, rp = _array(mean_out, (rows,), f32, dev, "mean_out"), _array(rstd_out, (rows,), f32, dev, "rstd_out")
     _call(lib.tm_layer_norm, dev, x.data_ptr(), ld, _ptr(residual), ld_r, code, rows, cols, wp, bp, wcode, eps, _ptr(sum_out), ld_s,
           y.data_ptr(), ld_y, mp, rp)
+    if cols == 0:                                           # of which the entry writes nothing
+        for t in (mean_out, rstd_out):
+            if t is not None:
+                t.fill_(float("nan"))
     return y, sum_out, mean_out, rstd_out
 
 

@@ -26,3 +26,15 @@ def test_few_and_many_wide_rows(rows, cols, residual):
     assert np.all(np.abs(f(y) - yd) <= ref.norm_bounds(hd, sd, wd, bd, yd, "bf16"))
     assert np.all(np.abs(f(mean) - md) <= 64 * ref.U32 * top) and np.all(np.abs(f(rstd) - sd) <= 64 * ref.U32 * sd * (1 + top * sd))
     assert s is None if not residual else np.all(np.abs(f(s) - hd) <= (ref.U16 + ref.U32) * np.abs(hd))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_rows_without_columns(dtype):
+    """The mean and deviation of nothing are NaN, not what the memory held."""
+    x = torch.empty((5, 0), dtype=dtype, device="cuda")
+    mean, rstd = torch.zeros(5, device="cuda"), torch.zeros(5, device="cuda")
+    y, s, _, _ = tm.tm_layer_norm(x, residual=x, mean_out=mean, rstd_out=rstd)
+    assert y.shape == s.shape == (5, 0) and torch.isnan(mean).all() and torch.isnan(rstd).all()
+    dx, dw, db = tm.tm_layer_norm_backward(x, x, mean, rstd)
+    assert dx.shape == (5, 0) and dw.shape == db.shape == (0,)
+    assert tm.tm_layer_norm(x, want_stats=False)[0].shape == (5, 0)
