@@ -72,8 +72,8 @@ template <int DT> __device__ __forceinline__ float vector_max_nan(const uint4& u
 }
 
 // A row seen as 16-byte vectors that start on 16-byte boundaries: vector 0 begins `lead` elements before the row.  Only the
-// first and the last vector can reach past the row; they are accessed one element at a time, so that nothing outside the
-// row is touched whatever its alignment.
+// first and the last vector can reach past the row; RowPart gives their elements one at a time, so that nothing outside the row is
+// touched whatever its alignment.
 template <int DT> struct RowVectors {
     using T = typename RowType<DT>::T;
     static constexpr int V = RowType<DT>::kVec;
@@ -86,32 +86,6 @@ template <int DT> struct RowVectors {
         count = cols > 0 ? (cols + lead + V - 1) / V : 0;
     }
     __device__ __forceinline__ long long column(long long i) const { return i * V - lead; }      // of the vector's first element; may be negative
-    __device__ __forceinline__ bool full(long long i) const { return column(i) >= 0 && column(i) + V <= n; }
-    // the vector as stored; elements outside the row are -Inf
-    __device__ __forceinline__ uint4 load(long long i) const {
-        const long long c = column(i);
-        if (full(i)) return *reinterpret_cast<const uint4*>(base + c);
-        float v[V];
-#pragma unroll
-        for (int j = 0; j < V; ++j) v[j] = (c + j >= 0 && c + j < n) ? to_float(base[c + j]) : -INFINITY;
-        uint32_t w[4];
-        pack_words<DT, 4>(v, w);
-        return make_uint4(w[0], w[1], w[2], w[3]);
-    }
-    // stores the vector to another row of the same length; `aligned`: that row starts at the same distance from a boundary
-    __device__ __forceinline__ void store(void* row, bool aligned, long long i, const float* v) const {
-        T* out = static_cast<T*>(row);
-        const long long c = column(i);
-        if (aligned && full(i)) {
-            uint32_t w[4];
-            pack_words<DT, 4>(v, w);
-            __stcs(reinterpret_cast<uint4*>(out + c), make_uint4(w[0], w[1], w[2], w[3]));
-        } else {
-#pragma unroll
-            for (int j = 0; j < V; ++j)
-                if (c + j >= 0 && c + j < n) from_float(out + c + j, v[j]);
-        }
-    }
 };
 
 // The part [from, to) of a row's vectors (to <= its count) that one thread block works on: `inside` full vectors from `vec` on, at

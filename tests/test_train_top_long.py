@@ -24,3 +24,17 @@ def test_long_lists_of_many_short_rows(rows, vocab, k, dtype):
         assert np.array_equal(ids[r], i) and np.array_equal(values[r], v), r
     want = np.array([ref.log_sum_exp(x / 1.5) for x in exact])
     assert np.all(np.abs(lse - want) <= ref.sum_unit(vocab, np.abs(exact).max() / 1.5) + 2 * ref.U32 * np.abs(want))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_the_largest_vocabulary(dtype):
+    from tests.test_train_distill import _check_distill, _check_top, _matrix
+    rng = np.random.Generator(np.random.PCG64(1))
+    vocab, k, t = 1 << 22, 100, 1.5
+    z, zd = _matrix(rng.standard_normal((2, vocab), dtype=np.float32) * 2, dtype)
+    _check_top(z, zd, 200, t)
+    ids = np.stack([rng.permutation(vocab)[:k] for _ in range(2)]).astype(np.int32)
+    values = np.sort(rng.standard_normal((2, k)).astype(np.float32) + 9)[:, ::-1].copy()
+    lse = np.array([ref.log_sum_exp(x.astype(np.float64) / t) + 0.2 for x in values], np.float32)
+    for teacher_lse in (lse, None):
+        _check_distill(z, zd, values, ids, teacher_lse, None, t, 1.0, dtype, inplace=teacher_lse is None)
