@@ -122,10 +122,10 @@ def tm_layer_norm(x, weight=None, bias=None, eps: float = 1e-5, residual=None, y
     ld_r = ld_s = ld_y = cols
     if residual is not None:
         ld_r = _other(residual, "residual", x)
-        if sum_out is None and want_sum:
-            sum_out = _like(x)
     if sum_out is not None:
         ld_s = _other(sum_out, "sum_out", x)
+    elif residual is not None and want_sum:
+        sum_out = _like(x)
     if y is not None:
         ld_y = _other(y, "y", x)
     else:
