@@ -240,25 +240,27 @@ __device__ __forceinline__ void fetch_list(const DistillArgs& a, long long r, in
 }
 
 // What a block's listed logits add to the loss: sum p and sum p (z - z0), z0 the largest of them.  entropy, norm: the list's.
-struct ListSums { double mass, dot; float z0, entropy, norm; };
+struct ListSums { double dot; float mass, z0, entropy, norm; };
 
 // A row's loss, by one warp: sum p log p - sum p log q + p_rest (log p_rest - log q_rest), put together in 64 bits because the sums
-// nearly cancel: an offset that all logits share drops out of (z0 - R) before anything is rounded.  Lane c brings block c's ListSums (zeros
-// from C on; entropy and norm: those of any block).  The four logs are taken side by side in four lanes.  base: what the exponentials' sums are relative to, in units of the
-// temperature -- R base_unit, or R itself where `slow` -- and gap: how far the rest's reference lies below it.  Lane 0 returns the loss,
-// and the statistics.
-__device__ __forceinline__ float row_loss(float rest, const ListSums& l, bool slow, double inv_t, double base_unit, float R, float R_rest, float s_all,
-                                          float s_rest, float& lse, float& log_rest) {
+// nearly cancel: an offset that all logits share drops out of (z0 - R) before anything is rounded.  Lane c < C brings block c's ListSums
+// (entropy and norm: those of any block).  The four logs are taken side by side in four lanes.  The exponentials' sums are relative to
+// R base_unit in units of the temperature, or to R itself where `slow`; R_rest: the rest's reference.  Lane 0 returns the loss, and the statistics.
+__device__ __forceinline__ float row_loss(float rest, const ListSums& l, int C, bool slow, double inv_t, double base_unit, float R, float R_rest, float s_all, float s_rest,
+                                          float& lse, float& log_rest) {
     const int lane = threadIdx.x & 31;
     const double unit = slow ? inv_t : base_unit;
-    const double mass = warp_sum_double(l.mass);
     const double above = slow ? ((double)l.z0 - R) * inv_t : l.z0 * inv_t - R * base_unit;       // z0 / T - base
-    const double cross = warp_sum_double(l.dot * inv_t + (l.mass > 0.0 ? l.mass * above : 0.0));  // sum p (z / T - base)
-    const double g = log((double)(lane == 0 ? s_all : lane == 1 ? s_rest : lane == 2 ? rest : l.norm));
-    const double log_all = __shfl_sync(0xFFFFFFFFu, g, 0), log_s = __shfl_sync(0xFFFFFFFFu, g, 1), log_r = __shfl_sync(0xFFFFFFFFu, g, 2),
-                 log_n = __shfl_sync(0xFFFFFFFFu, g, 3);
+    float mass = l.mass;
+    double cross = l.dot * inv_t + (mass > 0.0f ? mass * above : 0.0);                           // sum p (z / T - base)
+    if (C > 1) {
+        mass = group_sum<32>(lane < C ? mass : 0.0f);
+        cross = warp_sum_double(lane < C ? cross : 0.0);
+    }
+    const double log_all = log((double)(lane == 0 ? s_all : lane == 1 ? s_rest : lane == 2 ? rest : l.norm));      // lane 0's
+    const double log_s = __shfl_sync(0xFFFFFFFFu, log_all, 1), log_r = __shfl_sync(0xFFFFFFFFu, log_all, 2), log_n = __shfl_sync(0xFFFFFFFFu, log_all, 3);
     const double log_rest_d = log_s - log_all - ((double)R - R_rest) * unit;
-    double loss = (double)__shfl_sync(0xFFFFFFFFu, l.entropy, 0) - mass * log_n - cross + mass * log_all;
+    double loss = (double)l.entropy - mass * log_n - cross + mass * log_all;
     if (rest > 0.0f && s_rest > 0.0f) loss += rest * (log_r - log_rest_d);
     if (s_rest != s_rest) loss = s_rest;
     lse = (float)(R * unit + log_all);
@@ -445,19 +447,20 @@ __global__ void __launch_bounds__(NT + 32, kBlocks<LOSS, NT>) distill_kernel(con
                 }
                 __syncwarp();
                 if (C > 1) cluster_sync(); else __syncthreads();
-                float2 of_list = make_float2(lowest(), 0.0f);
                 float top = lowest();
                 for (int i = lane; i < C * NW; i += 32) top = fmaxf(top, (C > 1 ? cluster_load2(&part[turn][i % NW], i / NW) : part[turn][i]).x);
-                if (lane < C) of_list = C > 1 ? cluster_load2(&list_part[turn], lane) : list_part[turn];
                 sums.R_rest = group_max<32>(top);
-                sums.R_list = group_max<32>(of_list.x);
                 float sum = 0.0f;
                 for (int i = lane; i < C * NW; i += 32) {
                     const float2 v = C > 1 ? cluster_load2(&part[turn][i % NW], i / NW) : part[turn][i];
                     sum += v.y * exp2_fast(v.x - sums.R_rest);
                 }
                 sums.s_rest = group_sum<32>(sum);
-                sums.s_list = group_sum<32>(of_list.y * exp2_fast(of_list.x - sums.R_list));
+                if (C > 1) {
+                    const float2 of_list = lane < C ? cluster_load2(&list_part[turn], lane) : make_float2(lowest(), 0.0f);
+                    sums.R_list = group_max<32>(of_list.x);
+                    sums.s_list = group_sum<32>(of_list.y * exp2_fast(of_list.x - sums.R_list));
+                } else { sums.R_list = list_part[turn].x; sums.s_list = list_part[turn].y; }
                 turn ^= 1;
             };
             // listed elements of a vector become -Inf
@@ -525,7 +528,8 @@ __global__ void __launch_bounds__(NT + 32, kBlocks<LOSS, NT>) distill_kernel(con
                 m = fmaxf(m, z0 * c2);
                 z0 = group_max<32>(z0);
                 if (!(z0 > -INFINITY)) z0 = 0.0f;
-                double mass = 0.0, dot = 0.0;
+                float mass = 0.0f;
+                double dot = 0.0;
 #pragma unroll
                 for (int e = 0; e < kEntries; ++e) {
                     if (e * 32 >= slots) break;
@@ -535,9 +539,9 @@ __global__ void __launch_bounds__(NT + 32, kBlocks<LOSS, NT>) distill_kernel(con
                         dot += (double)list.p[e] * ((double)z[e] - z0);
                     }
                 }
-                mass = warp_sum_double(mass);
+                mass = group_sum<32>(mass);
                 dot = warp_sum_double(dot);
-                if (lane == 0) { rest_s = list.rest; list_sums[turn] = {mass, dot, z0, list.entropy, list.norm}; }
+                if (lane == 0) { rest_s = list.rest; list_sums[turn] = {dot, mass, z0, list.entropy, list.norm}; }
             } else {
                 float2 add = make_float2(0.0f, 0.0f);
                 const float2 cc = make_float2(c2, c2);
@@ -600,12 +604,11 @@ __global__ void __launch_bounds__(NT + 32, kBlocks<LOSS, NT>) distill_kernel(con
                 ListSums l = *from;
                 if (C > 1) {
                     const uint32_t c = lane < C ? lane : 0;
-                    l.mass = cluster_load_double(&from->mass, c);
+                    l.mass = cluster_load_float(&from->mass, c);
                     l.dot = cluster_load_double(&from->dot, c);
                     l.z0 = cluster_load_float(&from->z0, c);
                 }
-                if (lane >= C) l.mass = l.dot = 0.0;
-                const float loss = row_loss(rest, l, k.slow, plan.inv_t_d, plan.kappa * kLn2D, k.R, sums.R_rest, s_all, sums.s_rest, lse, log_rest);
+                const float loss = row_loss(rest, l, C, k.slow, plan.inv_t_d, plan.kappa * kLn2D, k.R, sums.R_rest, s_all, sums.s_rest, lse, log_rest);
                 if (lane == 0) {
                     a.loss[r] = loss * weight * a.scale;
                     if (!GRAD && a.stats) { a.stats[2 * r] = lse; a.stats[2 * r + 1] = a.teacher_lse ? log_rest : 0.0f; }
