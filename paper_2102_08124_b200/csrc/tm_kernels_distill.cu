@@ -294,12 +294,14 @@ struct RowPlan {
 };
 
 constexpr int kBlockVectors = 4;                   // vectors of a thread's block
-// Blocks an SM, that is the registers a thread may use: as many as do without spills in the loops (the loss of 2048 x 32001 fp32 takes
-// 65 us with three blocks of 256 threads and 67 with four, the gradient alone in bf16 58.7 and 54.4)
-template <bool LOSS, int NT> constexpr int kBlocks = NT == 512 ? 2 : NT == 256 ? (LOSS ? 3 : 4) : 8;
+// Blocks an SM, that is the registers a thread may use.  256 threads: the loss of 2048 x 32001 fp32 takes 65 us with three blocks and 67 with
+// four, the gradient alone in bf16 58.7 and 54.4.  128 threads, six blocks and eight (ptxas then spills 410 bytes of the loss, and 48 to 52
+// of the two other forms): the loss of 4000 x 4000 fp32 32.8 and 34.7 us, 4096 x 8000 bf16 42.0 and 43.0, but 4096 x 1000 bf16, whose time
+// is the list's, 33.4 and 32.5; loss and gradient 46.1 and 39.8, 55.9 and 51.5; the gradient alone of 4096 x 8000 bf16 37.9 and 35.8.
+template <bool LOSS, bool GRAD, int NT> constexpr int kBlocks = NT == 512 ? 2 : NT == 256 ? (LOSS ? 3 : 4) : LOSS && !GRAD ? 6 : 8;
 
 template <int DT, bool LOSS, bool GRAD, int NT>
-__global__ void __launch_bounds__(NT + 32, kBlocks<LOSS, NT>) distill_kernel(const DistillArgs a, const RowPlan plan) {
+__global__ void __launch_bounds__(NT + 32, kBlocks<LOSS, GRAD, NT>) distill_kernel(const DistillArgs a, const RowPlan plan) {
     using T = typename RowType<DT>::T;
     constexpr int V = RowType<DT>::kVec, NW = NT / 32, U = kBlockVectors;
     extern __shared__ __align__(16) uint8_t dynamic[];
@@ -692,7 +694,7 @@ template <int DT, bool LOSS, bool GRAD, int NT> cudaError_t launch_rows(const Di
 
 template <int DT, bool LOSS, bool GRAD, int NT> cudaError_t launch_as(const DistillArgs& a, RowPlan plan, cudaStream_t stream) {
     // a block's share of an SM's 228 KB for the stash, less its flags and static arrays
-    constexpr int kBlockBytes = NT * kBlockVectors * 16, kShare = 226 * 1024 / kBlocks<LOSS, NT> - 9 * 1024;
+    constexpr int kBlockBytes = NT * kBlockVectors * 16, kShare = 226 * 1024 / kBlocks<LOSS, GRAD, NT> - 9 * 1024;
     plan.stash = LOSS && GRAD ? std::max(0, std::min(plan.slice_vectors / (NT * kBlockVectors), (kShare - plan.flags) / kBlockBytes)) : 0;
     return launch_rows<DT, LOSS, GRAD, NT>(a, plan, stream);
 }
