@@ -5,13 +5,16 @@
 //              dw = sum_rows dy xh;  db = sum_rows dy
 //
 // Bound: HBM by bytes (8 respectively 14 operations an element against 4 to 16 bytes); as measured the latency of a row's loads and
-// reductions, after the number of instructions was halved (backward, 16384 x 1024 bf16: from 25.0 to 13.3 million warp instructions): two
-// elements an instruction wherever there is a packed form, parameters in registers over all rows, nothing worked out twice.
+// reductions, after the number of instructions was cut (backward, 16384 x 1024 bf16: from 25.0 to 13.3 million warp instructions; 16.4 with
+// the next row asked for ahead, which is faster): two elements an instruction wherever there is a packed form, parameters in registers
+// over all rows, nothing worked out twice.
 // A row belongs to a group of threads -- 8 or 32 of a warp, or up to 1024, by its width -- and stays in their registers between the
 // reductions and the output: it is read once.  Groups go through the rows with a stride and ask for the next row before they
 // reduce this one; several groups an SM cover each other's latency.
-// Measured, copy bandwidth 6.55 TB/s: forward with residual and sum 16384 x 1024 bf16 23.1 us (5.8 TB/s), 8000 x 4096 bf16 27.1 us
-// (4.8), 4097 x 1001 fp32 7.8 us (4.2); backward 16384 x 1024 bf16 with dsum 33.1 us (4.1), fp32 36.3 us (5.6), 2047 x 8191 bf16 57.0 us.
+// Measured in a replayed graph, copy bandwidth 6.55 TB/s, fp32 weights: forward with residual and sum 16384 x 1024 bf16 23.1 us (5.8 TB/s),
+// without them 8000 x 4096 bf16 26.1 us (5.0), 4097 x 1001 fp32 7.6 us (4.3), 2047 x 8191 bf16 22.5 us (3.0; with bf16 weights 25.8),
+// 2000 x 20000 bf16 135 us; backward 16384 x 1024 bf16 with dsum 32.9 us (4.1), fp32 36.2 us (5.6), 2047 x 8191 bf16 54.0 us (1.9; with bf16
+// weights 57.0), 2000 x 20000 bf16 242 us.  The figures at the forms below are of weights of the matrix's type.
 // The centred squares are summed after the mean is known (no difference of large numbers); the normalised value uses the sum
 // before it is rounded for sum_out: one rounding, at the end.
 // A thread owns the same columns of every row, so the backward pass keeps its share of dw and db in registers over all rows
@@ -442,7 +445,7 @@ __global__ void __launch_bounds__(kBackwardThreads<TPR, E>, kBackwardBlocks<TPR,
 }
 
 // Rows of 8193 to kRingWidth columns: two rows' inputs do not fit the registers beside the parameters' gradients, so bulk copies bring the
-// next rows to shared memory.  2000 x 16384 bf16 86 us, 3000 x 9000 fp32 85 us; with every step read from L2 again 198 and 186 us.  For
+// next rows to shared memory.  2000 x 16384 bf16 86 us, 3000 x 9000 fp32 86 us; with every step read from L2 again 198 and 186 us.  For
 // narrower rows the registers are faster: 16384 x 1024 bf16 77 us by this kernel, 32.7 us by the one above.
 // streams: dy, h and, with a third one, dsum
 constexpr int kRingThreads = 512;
