@@ -82,7 +82,8 @@ __device__ __forceinline__ Scale scale_of_stats(float lse, float log_rest, float
 constexpr float kFarLse = 1024.0f;
 
 // The sums of a whole row in logits, by all threads of a block; listed logits are told by their ids in the table (kHash words of -1, left
-// so).  For the few rows whose statistics are not enough.
+// so).  For the few rows whose statistics are not enough: it goes through them an element a thread (were all rows of 2048 x 32001 such, the
+// gradient would take 433 us in fp32 and 368 in bf16, instead of 94 and 54).
 template <int DT, int THREADS> __device__ __noinline__ Sums sums_of_row(const typename RowType<DT>::T* base, int n, const int* ids, int slots, int* hash, float c2, Sums* part) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const auto slot_of = [](int id) { return (int)(((uint32_t)id * 2654435769u) >> 23); };

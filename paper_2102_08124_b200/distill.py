@@ -47,18 +47,22 @@ def _make():
             if residual is not None and residual.shape != x.shape:       # rows of other shapes could still be as many
                 raise tm.TmError(2, "residual must have the shape of x")
             x2 = _rows(x)
-            y, h, mean, rstd = tt.tm_layer_norm(x2, weight, bias, eps, residual=None if residual is None else _rows(residual))
-            h = x2 if residual is None else h
-            ctx.save_for_backward(h, mean, rstd, weight)
+            # outputs of x's shape, of which the kernel gets views: a view itself could not be written to in place
+            y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+            h = None if residual is None else torch.empty_like(y)
+            _, _, mean, rstd = tt.tm_layer_norm(x2, weight, bias, eps, residual=None if residual is None else _rows(residual), y=y.view(x2.shape),
+                                                sum_out=None if h is None else h.view(x2.shape))
+            ctx.save_for_backward(x2 if h is None else h, mean, rstd, weight)
             ctx.shape, ctx.params = x.shape, (weight is not None or bias is not None, bias.dtype if bias is not None else None)
             ctx.set_materialize_grads(False)
             # without a residual the sum is x itself, whose other uses reach x by their own way
-            return y.view(x.shape), None if residual is None else h.view(x.shape)
+            return y, h
 
         @staticmethod
         @once_differentiable
         def backward(ctx, dy, dsum):
             h, mean, rstd, weight = ctx.saved_tensors
+            h = h.view(-1, h.shape[-1])
             want = ctx.params[0] and any(ctx.needs_input_grad[2:4])
             dsum = None if dsum is None else _rows(dsum)
             if dy is None:                                  # only the sum was used

@@ -126,3 +126,23 @@ def test_distill_gradients_in_bf16(tail):
     assert bool(((loss - want).abs() <= unit * (2 + reach) * scale).all())
     size = Z.grad.abs() + (scale / t * up * weight).double()[:, None] * (logq.detach().exp() + torch.zeros_like(logq).scatter_(1, at, logp.exp()))
     assert bool(((z.grad.reshape(rows, vocab).double() - Z.grad).abs() <= 2.0 ** -8 * Z.grad.abs() + 2 * unit * size).all())
+
+
+@pytest.mark.parametrize("shape", [(4, 16), (2, 3, 16)])
+def test_outputs_can_be_written_to_in_place(shape):
+    """y is not needed for the gradient, so it may change; the sum is, so a change is noticed."""
+    x, r = (torch.randn(*shape, device="cuda", requires_grad=True) for _ in range(2))
+    c = torch.randn(*shape, device="cuda")
+    y, h = layer_norm(x, residual=r)
+    want = torch.autograd.grad((2 * y * c).sum() + h.sum(), (x, r))
+    y, h = layer_norm(x, residual=r)
+    y.mul_(2.0)
+    got = torch.autograd.grad((y * c).sum() + h.sum(), (x, r))
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    y, h = layer_norm(x, residual=r)
+    h.add_(1.0)
+    with pytest.raises(RuntimeError, match="inplace"):
+        (y * c).sum().backward()
+    with torch.no_grad():
+        y, h = layer_norm(x, residual=r)
+        h.add_(y)
