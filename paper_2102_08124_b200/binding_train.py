@@ -66,7 +66,7 @@ def _input(t, what):
         raise TmError(2, "%s must be a 2-D CUDA tensor" % what)
     rows, cols = t.shape
     step = t.stride()
-    if cols > 1 and step[1] != 1:
+    if cols > 1 and step[1] != 1 and rows > 0:
         raise TmError(2, "%s must have unit column stride" % what)
     return code, t.device, rows, cols, step[0] if rows > 1 else cols
 
@@ -77,7 +77,7 @@ def _other(t, what, like):
         raise TmError(2, "%s must have the shape, dtype and device of the input matrix" % what)
     rows, cols = t.shape
     step = t.stride()
-    if cols > 1 and step[1] != 1:
+    if cols > 1 and step[1] != 1 and rows > 0:
         raise TmError(2, "%s must have unit column stride" % what)
     return step[0] if rows > 1 else cols
 

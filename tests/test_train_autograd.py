@@ -146,3 +146,25 @@ def test_outputs_can_be_written_to_in_place(shape):
     with torch.no_grad():
         y, h = layer_norm(x, residual=r)
         h.add_(y)
+
+
+@pytest.mark.parametrize("rows", [0, 1, 5])
+def test_slices_and_no_rows(rows):
+    """Inputs whose rows are apart, gradients that are expanded, no rows at all."""
+    x, r = (torch.randn(rows, 48, device="cuda", requires_grad=True) for _ in range(2))
+    w = torch.randn(16, device="cuda", requires_grad=True)
+    y, h = layer_norm(x[:, 8:24], w, residual=r.reshape(rows, 3, 16)[:, 1])
+    (y.sum() + 2 * h.sum()).backward()
+    X, R, W = (t.detach().double().requires_grad_() for t in (x, r, w))
+    Y, H = _norm64(X[:, 8:24], R[:, 16:32], W, 0.0)
+    (Y.sum() + 2 * H.sum()).backward()
+    for got, want in ((x, X), (r, R), (w, W)):
+        assert got.grad.shape == want.grad.shape and torch.allclose(got.grad.double(), want.grad, rtol=0, atol=2e-4)
+    z = torch.randn(rows, 80, device="cuda", requires_grad=True)
+    lists = teacher_lists(torch.randn(rows, 50, device="cuda"), 5)
+    loss = distill_loss(z[:, 10:60], lists)
+    loss.sum().backward()
+    b = z.detach()[:, 10:60].clone().requires_grad_()
+    one = distill_backward(b * 1, lists)
+    assert torch.allclose(loss, one, rtol=1e-5, atol=1e-6) and torch.allclose(z.grad[:, 10:60], b.grad, rtol=0, atol=1e-6)
+    assert not z.grad[:, :10].any() and not z.grad[:, 60:].any()
