@@ -302,7 +302,8 @@ int tm_layer_norm_backward(const void* dy, int64_t ld_dy, const void* h, int64_t
  *   tm_distill_loss       loss_out[rows]; stats_out[rows][2] (may be NULL): log-sum-exp of logits / temperature, log q_rest (0 without
  *                         teacher_lse, -Inf without mass there)
  *   tm_distill_grad       dlogits, from the stats of tm_distill_loss on the same arguments, times grad_loss[row] (NULL: 1)
- *                         (rows whose log-sum-exp is not inside +-1024, where fp32 holds too little of it, are summed again from their logits)
+ *                         (rows whose log-sum-exp or log q_rest is not inside +-1024, where fp32 holds too little of it, are summed again
+ *                         from their logits)
  *   tm_distill_loss_grad  both in one pass over the logits, for a step whose gradient of the loss is known (1 per row; a factor goes into scale)
  * dlogits may lie on logits.
  * An offset that all logits of a row share changes neither loss nor gradient, whatever its size; teacher_lse and top_values / temperature

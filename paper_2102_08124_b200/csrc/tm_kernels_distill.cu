@@ -77,8 +77,8 @@ __device__ __forceinline__ Scale scale_of_stats(float lse, float log_rest, float
     return k;
 }
 
-// A log-sum-exp in fp32 is off by up to 2^-24 of itself, and so are then all q = exp(z / T - lse), relatively: beyond this one (2^-14) a row's
-// sums are taken again from its logits.
+// A log-sum-exp in fp32 is off by up to 2^-24 of itself, and so are then all q = exp(z / T - lse), relatively; the same goes for log q_rest and
+// q_j / q_rest.  Beyond this size of either (2^-14) a row's sums are taken again from its logits.
 constexpr float kFarLse = 1024.0f;
 
 // The sums of a whole row in logits, by all threads of a block; listed logits are told by their ids in the table (kHash words of -1, left
@@ -619,8 +619,9 @@ __global__ void __launch_bounds__(NT + 32, kBlocks<LOSS, GRAD, NT>) distill_kern
             }
         } else {
             rest = rest_s;
-            const float lse = a.stats[2 * r];
-            if (fabsf(lse) < kFarLse) k = scale_of_stats(lse, a.stats[2 * r + 1], rest, plan.unit);
+            const float lse = a.stats[2 * r], log_rest = a.stats[2 * r + 1];
+            const bool far_rest = rest > 0.0f && log_rest < -kFarLse && log_rest > -kMasked * (float)kLn2D;
+            if (fabsf(lse) < kFarLse && !far_rest) k = scale_of_stats(lse, log_rest, rest, plan.unit);
             else {
                 Sums sums = sums_of_row<DT, NT + 32>(row.base, (int)a.vocab, list_id, slots, hash, c2, far_part);
                 scale_of_sums(sums, rest, true, c2, k);

@@ -122,3 +122,27 @@ def test_gradients_on_the_logits_of_rows_with_an_offset(rows, vocab):
     assert float((want - both).abs().max()) <= 2 * ref.sum_unit(vocab, 40.0) + 2.0 ** -14  # q at most 1; the statistics' rounding inside +-1024
     again = z.clone()
     assert torch.equal(tm.tm_distill_grad(again, values, ids, stats, dlogits=again), want)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("t", [1.0, 0.25])
+@pytest.mark.parametrize("vocab", [301, 5000, 70000])
+@pytest.mark.parametrize("gap", [2048.0, 32768.0, 524288.0])                             # of z / T
+def test_masks_that_still_count(gap, vocab, t, dtype):
+    """Unlisted logits of one level, far below the listed ones: each gets an equal share of the teacher's remaining mass, by any of the entries."""
+    rng = np.random.Generator(np.random.PCG64(vocab))
+    rows, k = 3, 30
+    ids = np.stack([rng.permutation(vocab)[:k] for _ in range(rows)]).astype(np.int32)
+    v = (rng.standard_normal((rows, k)) + 3).astype(np.float32)
+    rest = np.array([0.05, 0.2, 0.5])
+    lse = (np.array([ref.log_sum_exp(x.astype(np.float64) / t) for x in v]) - np.log1p(-rest)).astype(np.float32)
+    z = np.full((rows, vocab), -gap * t)
+    np.put_along_axis(z, ids.astype(np.int64), rng.standard_normal((rows, k)), 1)
+    loss, loss2, stats, grad, grad2 = _run(torch.from_numpy(z.astype(np.float32)).to(DT[dtype]).cuda(), v, ids, lse, t, 1.0)
+    for r in range(rows):
+        p_rest = 1.0 - np.exp(v[r].astype(np.float64) / t - float(lse[r])).sum()
+        unit = ref.sum_unit(vocab, max(np.abs(v[r] / t).max(), abs(lse[r])))             # of p_rest, and of a sum of equal exponentials
+        out = np.setdiff1d(np.arange(vocab), ids[r])
+        want = -p_rest / t / (vocab - k)
+        for g in (grad[r, out], grad2[r, out]):
+            assert np.all(np.abs(g - want) <= (ref.out_unit(dtype) + 4 * ref.U32) * abs(want) + 4 * unit / t / (vocab - k)), (r, g[:3], want)
