@@ -298,7 +298,8 @@ int tm_layer_norm_backward(const void* dy, int64_t ld_dy, const void* h, int64_t
  * more than 2^20 binades of exp(logit / temperature) below the listed ones, which only masks are (the type's lowest value, say).  Finite
  * gaps below that count in full, however small q_rest is.  An entry whose id is negative is padding (lists of different lengths); one
  * whose id is not below vocab, or stood in the row before, is left out too and raises TM_DEV_BADID in *status_dev.
- * A row of weight 0, or without entries, has loss 0 and gradient 0 whatever its logits hold.  0 <= k <= TM_TOP_MAX.
+ * A row of weight 0, or without entries, has loss 0 and gradient 0 whatever its logits hold.  A row of another weight whose
+ * teacher's entries are all -Inf has NaN for both, as their softmax.  0 <= k <= TM_TOP_MAX.
  *   tm_distill_loss       loss_out[rows]; stats_out[rows][2] (may be NULL): log-sum-exp of logits / temperature, log q_rest (0 without
  *                         teacher_lse, -Inf without mass there)
  *   tm_distill_grad       dlogits, from the stats of tm_distill_loss on the same arguments, times grad_loss[row] (NULL: 1)
