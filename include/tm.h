@@ -324,6 +324,69 @@ int tm_distill_loss_grad(const void* logits, int dtype, int64_t rows, int64_t vo
                          const float* teacher_lse, const float* row_weight, float temperature, float scale, float* loss_out, void* dlogits,
                          int64_t ld_d, int* status_dev, void* cuda_stream);
 
+/*
+ * The residual branch.  Random numbers come from a counter, Philox4x32 with ten rounds: key = the two halves of seed, counter = (block, row, the two
+ * halves of offset + *offset_dev), low halves first.  offset_dev (device memory, may be NULL: 0) is read when the kernel runs, so that a
+ * captured graph draws other numbers at every replay.  Whoever wants other numbers gives another seed or offset.
+ *
+ * tm_dropout -- y = d(x) + residual (residual NULL: y = d(x)), with d(x) = x / (1 - p') where an element stays and 0 where it is dropped
+ * (an Inf or NaN too).  Block c / 8 of row r holds 16 bits for each of eight columns, low half of the first word first: column c stays where its
+ * bits are not below 65536 p', p' = round(65536 p) / 65536 (at most 65535 / 65536), 0 <= p < 1.  Nothing is stored: the gradient of x is
+ * tm_dropout(dy) with the same numbers, that of residual is dy.  y may lie on x or residual.  rows up to 2^32 - 1, cols up to 2^35.
+ *
+ * tm_rms_norm -- h = d(x) + residual (p = 0: d(x) = x; residual NULL: none); over the columns of every row
+ * rstd = 1 / sqrt(mean(h^2) + eps), y = h * rstd * weight (cols entries of weight_dtype, NULL for ones).  sum_out (may be NULL) receives h
+ * rounded to dtype, rstd_out (rows floats, may be NULL) rstd; y comes from h before rounding.  y or sum_out may lie on x or residual.
+ * With cols 0 nothing is written.
+ *
+ * tm_rms_norm_e4m3 -- the same without dropout, y in 8 bits (e4m3: four bits of exponent, three of mantissa, largest value 448) with a scale for
+ * every `group` columns of a row (32, 64 or 128; the last may have fewer; 0: one for the row): scale = max(max |y| / 448, 2^-126),
+ * y8 = y / scale rounded to nearest even; y is scale * y8.  scales_out[rows][ceil(cols / group)] (group 0: [rows]).  NaN stays NaN in y8 and has no
+ * part in the scale.  sum_out may lie on x or residual, y8 on neither.
+ *
+ * tm_rms_norm_backward -- with g = dy * weight and xh = h * rstd:
+ *   dh = rstd * (g - xh * mean_c(g * xh)) + dsum,   dx = d(dh) (the forward pass's p, seed and offsets),   dweight = sum_r(dy * xh).
+ * h is the forward pass's x (without dropout and residual) or its sum_out; dh is the gradient of the sum and so of the residual, dx that of x; either
+ * may be NULL.  dsum (may be NULL) is a gradient that reaches h by another way.  dweight_out (cols entries of weight_dtype, may be NULL) is
+ * written, not added to, and needs a workspace of tm_rms_norm_workspace_bytes(rows, cols) bytes, 256-byte aligned.
+ * dh and dx may lie on dy, h or dsum, but not on each other.
+ */
+int tm_dropout(const void* x, int64_t ld_x, const void* residual, int64_t ld_residual, int dtype, int64_t rows, int64_t cols, double p,
+               uint64_t seed, uint64_t offset, const uint64_t* offset_dev, void* y, int64_t ld_y, void* cuda_stream);
+int tm_rms_norm(const void* x, int64_t ld_x, const void* residual, int64_t ld_residual, int dtype, int64_t rows, int64_t cols,
+                const void* weight, int weight_dtype, float eps, double p, uint64_t seed, uint64_t offset, const uint64_t* offset_dev,
+                void* sum_out, int64_t ld_sum, void* y, int64_t ld_y, float* rstd_out, void* cuda_stream);
+int tm_rms_norm_e4m3(const void* x, int64_t ld_x, const void* residual, int64_t ld_residual, int dtype, int64_t rows, int64_t cols,
+                     const void* weight, int weight_dtype, float eps, int group, void* sum_out, int64_t ld_sum, void* y8, int64_t ld_y8,
+                     float* scales_out, float* rstd_out, void* cuda_stream);
+size_t tm_rms_norm_workspace_bytes(int64_t rows, int64_t cols);
+int tm_rms_norm_backward(const void* dy, int64_t ld_dy, const void* h, int64_t ld_h, int dtype, int64_t rows, int64_t cols,
+                         const void* weight, int weight_dtype, const float* rstd, const void* dsum, int64_t ld_dsum,
+                         double p, uint64_t seed, uint64_t offset, const uint64_t* offset_dev, void* dh, int64_t ld_dh, void* dx, int64_t ld_dx,
+                         void* dweight_out, void* workspace_dev, size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * tm_verify_draft -- tokens that a drafter proposed, checked against the target's probabilities so that what comes out is distributed as the
+ * target's own tokens.  logits: batch * (drafted + 1) rows, row b (drafted + 1) + i the target's after i drafts of sequence b; draft_logits: batch *
+ * drafted rows, row b drafted + i what draft i was drawn from (NULL: the drafter was certain, q = 1 for the draft and 0 for all else);
+ * draft_ids[batch][drafted], a negative id ends a sequence's drafts.  With p = softmax(logits / temperature) and
+ * q = softmax(draft_logits / draft_temperature): draft i stays while u_i q(id) < p(id).  Behind the last that stays one more token
+ * is drawn: from max(p - q, 0) where a draft was refused (from p, should that be zero everywhere), else from p.  It is the k with the largest
+ * r_k / -log(1 - u_k), the lower one of equals: each k wins with probability r_k / sum r.
+ *   tokens_out[batch][drafted + 1]   the drafts that stayed, the drawn token, and -1 behind it
+ *   accepted_out[batch]              how many drafts stayed
+ *   logp_out[batch][drafted + 1]     log p of these tokens (may be NULL), 0 behind them
+ * Random numbers (see above): u = (word + 1/2) / 2^32; the draw takes word k % 4 of block k / 4 of row b, the test of draft i word i % 4 of block
+ * 2^31 + i / 4.  With drafted 0 a call draws one token a row from softmax(logits / temperature).
+ * -Inf (a masked logit) has probability 0.  A row that is reached and holds NaN, +Inf or nothing but -Inf ends its sequence with
+ * token -1 and logp NaN and raises TM_DEV_NONFINITE in *status_dev (may be NULL); an id that is not below vocab ends the drafts like a negative
+ * one and raises TM_DEV_BADID.  Rows behind the first refused draft are not read.  1 <= vocab <= TM_VOCAB_MAX, 0 <= drafted <= TM_DRAFT_MAX.
+ */
+#define TM_DRAFT_MAX 1024
+int tm_verify_draft(const void* logits, int dtype, int64_t batch, int64_t drafted, int64_t vocab, int64_t ld, const void* draft_logits,
+                    int64_t ld_draft, const int32_t* draft_ids, float temperature, float draft_temperature, uint64_t seed, uint64_t offset,
+                    const uint64_t* offset_dev, int32_t* tokens_out, int32_t* accepted_out, float* logp_out, int* status_dev, void* cuda_stream);
+
 const char* tm_status_string(int code);
 int tm_version(void);
 

@@ -15,3 +15,6 @@ from .binding_train import (  # noqa: F401
     TM_DEV_BADID, TM_ERR_RANGE, TM_TOP_MAX, tm_layer_norm, tm_layer_norm_backward, tm_layer_norm_workspace_bytes, tm_top_logits,
     tm_distill_loss, tm_distill_grad, tm_distill_loss_grad,
 )
+from .binding_branch import (  # noqa: F401
+    TM_DRAFT_MAX, tm_dropout, tm_rms_norm, tm_rms_norm_backward, tm_rms_norm_e4m3, tm_rms_norm_workspace_bytes, tm_verify_draft,
+)

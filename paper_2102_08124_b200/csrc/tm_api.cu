@@ -641,7 +641,7 @@ const char* tm_status_string(int code) {
     case TM_ERR_WORKSPACE: return "workspace missing, misaligned or too small";
     case TM_ERR_TOO_LARGE: return "too many matrices for the built-in scratch (TM_STATIC_MAX_MATRICES per call)";
     case TM_ERR_CAPTURE: return "the stream is being captured and the call would have to copy descriptor tables from host memory (use tm_plan_run)";
-    case TM_ERR_RANGE: return "a scalar is out of range (list length, temperature, eps or scale)";
+    case TM_ERR_RANGE: return "a scalar is out of range (list length, temperature, eps, scale, share to drop or group)";
     default: return "unknown status";
     }
 }

@@ -142,6 +142,60 @@ struct DistillArgs {                            // tm_kernels_distill.cu
 };
 cudaError_t launch_distill(const DistillArgs& a, int dtype, bool loss, bool grad, int sms, cudaStream_t stream);
 
+// Dropout from the counter-based generator of tm_philox.cuh: an element stays where its 16 bits are `limit` or more (0: there is none), times `scale`.
+struct DropSpec {
+    uint32_t limit;
+    float scale;                                // 65536 / (65536 - limit)
+    unsigned long long seed, offset;
+    const unsigned long long* offset_dev;       // or null; added to offset
+};
+// The residual branch (tm_kernels_rms.cu)
+struct DropoutArgs {
+    const void *x, *residual;                   // residual or null
+    long long rows, cols, ld_x, ld_residual, ld_y;
+    DropSpec drop;
+    void* y;
+};
+struct RmsArgs {
+    const void *x, *residual;                   // residual or null
+    long long rows, cols, ld_x, ld_residual, ld_sum, ld_y;
+    const void* weight;                         // or null
+    bool weight_f32, weight_vec;                // fp32 (else bf16); may be read 16 bytes at a time (set by the launch)
+    float eps;
+    DropSpec drop;
+    void *sum, *y;                              // sum or null; y of the matrix's type, or e4m3 (one byte an element) where scales are written
+    float *rstd, *scales;                       // or null
+    int group;                                  // columns that share a scale: 32, 64, 128, or 0 for a whole row
+};
+struct RmsBackArgs {
+    const void *dy, *h, *dsum;                  // dsum or null
+    long long rows, cols, ld_dy, ld_h, ld_dsum, ld_dh, ld_dx;
+    const void* weight;                         // or null
+    bool weight_f32, weight_vec;
+    const float* rstd;
+    DropSpec drop;
+    void *dh, *dx;                              // one of them or both
+    float* partials;                            // rms_partial_rows() rows of cols floats, or null
+};
+int rms_partial_rows(long long rows, long long cols);
+cudaError_t launch_dropout(const DropoutArgs& a, int dtype, int sms, cudaStream_t stream);
+cudaError_t launch_rms_forward(RmsArgs a, int dtype, int sms, cudaStream_t stream);
+cudaError_t launch_rms_backward(RmsBackArgs a, int dtype, void* dweight, int sms, cudaStream_t stream);
+
+struct VerifyArgs {                             // tm_kernels_verify.cu
+    const void *logits, *draft_logits;          // draft_logits null: a draft's own probability is 1
+    long long vocab, ld, ld_draft;
+    int batch, drafted;
+    const int* ids;
+    float temperature, draft_temperature;
+    unsigned long long seed, offset;
+    const unsigned long long* offset_dev;       // or null
+    int *tokens, *accepted;
+    float* logp;                                // or null
+    int* status;                                // or null
+};
+cudaError_t launch_verify(const VerifyArgs& a, int dtype, int sms, cudaStream_t stream);
+
 // The current device's number of multiprocessors (looked up once per device); a TM_* code.
 int device_sms(int* sms);
 
