@@ -89,21 +89,371 @@ __device__ __forceinline__ void store_e4m3(uint8_t* row, long long c, long long 
 // A group's scale from its largest magnitude; NaN does not count (it stays in the values), and no scale is zero
 __device__ __forceinline__ float scale_of(float most) { return fmaxf(most * (1.0f / kMostE4m3), kLeastScale); }
 
-template <int DT, bool VEC> __global__ void __launch_bounds__(256) dropout_kernel(const DropoutArgs a) {
+// x / d rounded down for x below 2^31, by a product: m = ceil(2^(31 + bits) / d) with d <= 2^bits
+struct Divide {
+    uint32_t d, m, shift;
+    explicit Divide(uint32_t d_) : d(d_) {
+        uint32_t bits = 0;
+        while (bits < 31 && (1u << bits) < d) ++bits;
+        shift = bits;
+        m = (uint32_t)(((1ull << (31 + bits)) + d - 1) / d);
+    }
+    __device__ __forceinline__ uint32_t operator()(uint32_t x) const { return (uint32_t)(((unsigned long long)x * m) >> (31 + shift)); }
+};
+
+// A thread a block of eight columns (16 bytes of bf16; twice that of fp32, the last half perhaps past the row), kEach of them at a time
+constexpr int kDropThreads = 256, kDropBlocks = 5;
+template <int DT, bool DROP> __global__ void __launch_bounds__(kDropThreads, kDropBlocks) dropout_kernel(const DropoutArgs a, const Divide by, uint32_t all) {
+    constexpr int kEach = DT == kBF16 ? 2 : 1, V = RowType<DT>::kVec, N = 8 / V;
     const PhiloxKey key(a.drop.seed, a.drop.offset, a.drop.offset_dev);
-    const long long blocks = (a.cols + 7) / 8, all = a.rows * blocks;
-    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < all; i += (long long)gridDim.x * 256) {
-        const long long r = i / blocks, c = (i - r * blocks) * 8;
-        float v[8];
-        load_block<DT, VEC>(row_of<DT>(a.x, a.ld_x, r), c, a.cols, v);
-        if (a.drop.limit) drop_block(key, a.drop, r, c, v);
-        if (a.residual) {
-            float s[8];
-            load_block<DT, VEC>(row_of<DT>(a.residual, a.ld_residual, r), c, a.cols, s);
+    const uint32_t step = gridDim.x * kDropThreads, high = a.drop.limit << 16;
+    const int cols = (int)min(a.cols, (long long)INT32_MAX);
+    for (uint32_t i0 = blockIdx.x * kDropThreads + threadIdx.x; i0 < all; i0 += kEach * step) {
+        uint4 x[kEach][N], s[kEach][N];
+        uint32_t r[kEach], c[kEach];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] += s[j];
+        for (int k = 0; k < kEach; ++k) {
+            const uint32_t i = i0 + k * step;
+            r[k] = by(i);
+            c[k] = (i - r[k] * by.d) * 8;
+#pragma unroll
+            for (int q = 0; q < N; ++q) {
+                x[k][q] = s[k][q] = make_uint4(0, 0, 0, 0);
+                if (i < all && (int)c[k] + q * V < cols) {
+                    x[k][q] = *reinterpret_cast<const uint4*>(row_of<DT>(a.x, a.ld_x, r[k]) + c[k] + q * V);
+                    if (a.residual) s[k][q] = *reinterpret_cast<const uint4*>(row_of<DT>(a.residual, a.ld_residual, r[k]) + c[k] + q * V);
+                }
+            }
         }
-        store_block<DT, VEC>(row_of<DT>(a.y, a.ld_y, r), c, a.cols, v);
+#pragma unroll
+        for (int k = 0; k < kEach; ++k) {
+            const uint4 w = DROP ? key(c[k] / 8, r[k]) : make_uint4(0, 0, 0, 0);
+            const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+            for (int q = 0; q < N; ++q) {
+                float v[V], t[V];
+                unpack_vector<DT>(x[k][q], v);
+                unpack_vector<DT>(s[k][q], t);
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    const uint32_t word = u[(q * V + j) / 2];
+                    if (DROP) v[j] = (j & 1 ? word : word << 16) >= high ? v[j] * a.drop.scale : 0.0f;      // a dropped Inf or NaN is gone
+                    v[j] += t[j];
+                }
+                uint32_t o[4];
+                pack_words<DT, 4>(v, o);
+                if (i0 + k * step < all && (int)c[k] + q * V < cols)
+                    *reinterpret_cast<uint4*>(row_of<DT>(a.y, a.ld_y, r[k]) + c[k] + q * V) = make_uint4(o[0], o[1], o[2], o[3]);
+            }
+        }
+    }
+}
+// Rows that start anywhere, or more blocks than 32 bits count: a warp takes 256 columns of a row in eight accesses side by side.  Lane k
+// works out which columns of block k stay; a column's bit comes from there.
+template <int DT> __global__ void __launch_bounds__(kDropThreads) dropout_any_kernel(const DropoutArgs a) {
+    using T = typename RowType<DT>::T;
+    const PhiloxKey key(a.drop.seed, a.drop.offset, a.drop.offset_dev);
+    const long long parts = (a.cols + 255) / 256, all = a.rows * parts, step = (long long)gridDim.x * (kDropThreads / 32);
+    const int lane = threadIdx.x & 31;
+    for (long long i = (long long)blockIdx.x * (kDropThreads / 32) + (threadIdx.x >> 5); i < all; i += step) {
+        const long long r = i / parts, c0 = (i - r * parts) * 256;
+        const T *x = row_of<DT>(a.x, a.ld_x, r) + c0 + lane, *s = a.residual ? row_of<DT>(a.residual, a.ld_residual, r) + c0 + lane : nullptr;
+        T* y = row_of<DT>(a.y, a.ld_y, r) + c0 + lane;
+        const int left = (int)min(256ll, a.cols - c0) - lane;
+        float v[8], w[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            v[j] = 32 * j < left ? to_float(x[32 * j]) : 0.0f;
+            w[j] = s && 32 * j < left ? to_float(s[32 * j]) : 0.0f;
+        }
+        const uint32_t kept = a.drop.limit ? kept_bits(key((uint32_t)(c0 / 8) + lane, (uint32_t)r), a.drop.limit) : 0xFFu;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const uint32_t bits = __shfl_sync(0xFFFFFFFFu, kept, 4 * j + lane / 8);
+            if (32 * j < left) from_float(y + 32 * j, ((bits >> (lane & 7)) & 1u ? v[j] * a.drop.scale : 0.0f) + w[j]);
+        }
+    }
+}
+
+// ---- a row in registers --------------------------------------------------------------------------------------------
+
+constexpr int kPlain = 0, kDrop = 1, kE4m3 = 2;      // forms of the kernels below
+
+// Dropout of what TPR >= 32 threads hold of a row (RowRegs).  A warp's lanes work out one block of eight columns each; accesses
+// narrower than a block take their columns' bits from the lane that has them.
+template <int DT, int VB, int TPR, int E> __device__ __forceinline__ void drop_row(const PhiloxKey& key, const DropSpec& d, long long r, float2 (&v)[E / 2]) {
+    constexpr int VE = Access<DT, VB>::kElems, A = 8 / VE, B = 4 * VE;      // accesses and, in each of them, blocks that a warp's 32 blocks are
+    float* f = reinterpret_cast<float*>(v);
+    const int t = threadIdx.x % TPR, lane = threadIdx.x & 31;
+#pragma unroll
+    for (int k = 0; k < E / 8; ++k) {
+        const uint32_t block = (uint32_t)((k * A + lane / B) * (TPR * VE / 8) + (t - lane) * VE / 8 + lane % B);
+        const uint4 w = key(block, (uint32_t)r);
+        if constexpr (VE == 8) {
+            const uint32_t high = d.limit << 16, u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+            for (int j = 0; j < 8; ++j) f[8 * k + j] = (j & 1 ? u[j / 2] : u[j / 2] << 16) >= high ? f[8 * k + j] : 0.0f;
+        } else {
+            const uint32_t kept = kept_bits(w, d.limit);
+#pragma unroll
+            for (int i = 0; i < A; ++i) {
+                const uint32_t bits = __shfl_sync(0xFFFFFFFFu, kept, i * B + lane * VE / 8) >> (lane * VE & 7);
+#pragma unroll
+                for (int j = 0; j < VE; ++j) f[(k * A + i) * VE + j] = (bits >> j) & 1u ? f[(k * A + i) * VE + j] : 0.0f;
+            }
+        }
+    }
+    const float2 scale = make_float2(d.scale, d.scale);
+#pragma unroll
+    for (int k = 0; k < E / 2; ++k) v[k] = __fmul2_rn(v[k], scale);
+}
+
+// v times the parameters of its columns, an access after the other: rows whose parameters have no registers of their own
+template <int DT, int VB, int TPR, int E> __device__ __forceinline__ void times_params(const void* p, bool f32, bool vec, int cols, float2 (&v)[E / 2]) {
+    using R = RowRegs<DT, VB, TPR, E>;
+    float* f = reinterpret_cast<float*>(v);
+#pragma unroll
+    for (int i = 0; i < R::NV; ++i) {
+        float w[R::VE];
+        if (R::column(i) < cols) {
+            load_params<R::VE>(p, f32, vec, R::column(i), w, 1.0f);
+#pragma unroll
+            for (int j = 0; j < R::VE; ++j) f[i * R::VE + j] *= w[j];
+        }
+    }
+}
+
+// (sum of v.x, largest v.y) over the TPR threads of a row; buf as for row_sum2
+template <int TPR, int GROUPS> __device__ __forceinline__ float2 row_sum_max(float2 v, float2* buf) {
+    v = make_float2(group_sum<32>(v.x), group_max<32>(v.y));
+    if constexpr (TPR <= 32) return v;
+    else {
+        constexpr int W = TPR / 32;
+        if ((threadIdx.x & 31) == 0) buf[threadIdx.x >> 5] = v;
+        row_barrier<TPR, GROUPS>();
+        const float2 t = buf[(threadIdx.x / TPR) * W + (threadIdx.x & (W - 1))];
+        return make_float2(group_sum<W>(t.x), group_max<32>(t.y));
+    }
+}
+
+// Threads of a block whose rows are shared by TPR threads each, and blocks an SM
+template <int TPR> constexpr int kForwardThreads = TPR <= 32 ? 128 : TPR;
+template <int TPR, int E> constexpr int kForwardBlocks = std::max(1, (E <= 8 ? 1024 : 768) / kForwardThreads<TPR>);
+template <int TPR, int E> constexpr int kBackwardThreads = TPR <= 32 ? 128 : TPR <= 128 ? 384 : TPR <= 256 ? (E <= 8 ? 768 : 256) : TPR;
+template <int TPR, int E> constexpr int kBackwardBlocks = std::max(1, (E <= 8 ? 768 : 512) / kBackwardThreads<TPR, E>);
+
+template <int DT, int VB, int TPR, int E, int FORM>
+__global__ void __launch_bounds__(kForwardThreads<TPR>, kForwardBlocks<TPR, E>) rms_forward_kernel(const RmsArgs a, bool vec8) {
+    using R = RowRegs<DT, VB, TPR, E>;
+    constexpr int P = E / 2, VE = R::VE, kGroups = kForwardThreads<TPR> / TPR;
+    // kAhead: the next row is asked for before this one is reduced, where the registers suffice; kFetch: else it is brought to L2
+    constexpr bool kAhead = VB == 16 ? DT == kBF16 || R::NV <= 2 : E == 16 && (TPR == 256 || TPR == 512), kKeep = TPR < 1024 || E < 16, kFetch = !kAhead && TPR >= 128;
+    __shared__ float2 buf[2][32];
+    __shared__ float tops[FORM == kE4m3 && VE == 1 ? kGroups * TPR * E / 32 : 1];
+    const PhiloxKey key(a.drop.seed, a.drop.offset, FORM == kDrop ? a.drop.offset_dev : nullptr);
+    const int t = threadIdx.x % TPR, g = threadIdx.x / TPR, cols = (int)a.cols, lane = threadIdx.x & 31;
+    const float inv_n = 1.0f / (float)a.cols;
+    const long long step = (long long)gridDim.x * kGroups;
+    float2 w[P];
+    if constexpr (kKeep) R::params(a.weight, a.weight_f32, a.weight_vec, cols, w, 1.0f);
+    typename R::Raw ux[R::NV], us[R::NV];
+    const auto ask = [&](long long r) {
+        if constexpr (kAhead) {
+            const int n = r < a.rows ? cols : 0;
+            R::ask(row_of<DT>(a.x, a.ld_x, r), n, ux);
+            if (a.residual) R::ask(row_of<DT>(a.residual, a.ld_residual, r), n, us);
+        }
+    };
+    ask((long long)blockIdx.x * kGroups + g);
+    int turn = 0;
+    for (long long r0 = (long long)blockIdx.x * kGroups; r0 < a.rows; r0 += step, turn ^= 1) {
+        const long long r = r0 + g;
+        const bool on = r < a.rows;                       // whole groups idle together, but take part in the shuffles and barriers
+        float2 h[P];
+        if constexpr (kAhead) R::take(ux, h);
+        else R::load(row_of<DT>(a.x, a.ld_x, r), on ? cols : 0, h);
+        if constexpr (FORM == kDrop) drop_row<DT, VB, TPR, E>(key, a.drop, r, h);
+        if (a.residual) {
+            float2 s[P];
+            if constexpr (kAhead) R::take(us, s);
+            else R::load(row_of<DT>(a.residual, a.ld_residual, r), on ? cols : 0, s);
+#pragma unroll
+            for (int k = 0; k < P; ++k) h[k] = __fadd2_rn(h[k], s[k]);
+        }
+        ask(r + step);
+        if constexpr (kFetch) R::fetch(a.x, a.ld_x, a.residual ? a.residual : a.x, a.residual ? a.ld_residual : a.ld_x, r + step, a.rows, cols);
+        if (a.sum && on) R::store(row_of<DT>(a.sum, a.ld_sum, r), cols, h);
+        float2 sq = make_float2(0.0f, 0.0f);
+        float top = 0.0f;
+#pragma unroll
+        for (int k = 0; k < P; ++k) sq = __ffma2_rn(h[k], h[k], sq);
+        if constexpr (!kKeep) times_params<DT, VB, TPR, E>(a.weight, a.weight_f32, a.weight_vec, cols, h);
+#pragma unroll
+        for (int k = 0; k < P; ++k) {
+            if constexpr (kKeep) h[k] = __fmul2_rn(h[k], w[k]);      // zeros past the last column
+            if constexpr (FORM == kE4m3) top = fmaxf(top, fmaxf(fabsf(h[k].x), fabsf(h[k].y)));
+        }
+        float rstd;
+        if constexpr (FORM == kE4m3) {
+            const float2 both = row_sum_max<TPR, kGroups>(make_float2(sq.x + sq.y, top), buf[turn]);
+            rstd = 1.0f / sqrtf(both.x * inv_n + a.eps);
+            top = both.y;
+        } else rstd = 1.0f / sqrtf(row_sum<TPR, kGroups>(sq.x + sq.y, reinterpret_cast<float*>(buf[turn])) * inv_n + a.eps);
+        if (t == 0 && on && a.rstd) a.rstd[r] = rstd;
+        if constexpr (FORM != kE4m3) {
+            if (!on) continue;
+            const float2 rr = make_float2(rstd, rstd);
+#pragma unroll
+            for (int k = 0; k < P; ++k) h[k] = __fmul2_rn(h[k], rr);
+            R::store(row_of<DT>(a.y, a.ld_y, r), cols, h);
+        } else {
+            const float* f = reinterpret_cast<const float*>(h);
+            uint8_t* y = static_cast<uint8_t*>(a.y) + r * a.ld_y;
+            float* scales = a.scales + r * (a.group ? (cols + a.group - 1) / a.group : 1);
+            float scale = scale_of(top * rstd);
+            if (a.group == 0 && t == 0 && on) scales[0] = scale;
+            if (VE == 1 && a.group) {                     // a warp's accesses are 32 columns each
+                float* mine = tops + g * (TPR * E / 32);
+#pragma unroll
+                for (int i = 0; i < R::NV; ++i) {
+                    const float m = group_max<32>(fabsf(f[i]));
+                    if (lane == 0) mine[(i * TPR + t) / 32] = m;
+                }
+                row_barrier<TPR, kGroups>();               // the next row's writes come behind its reduction, which waits for these reads
+            }
+#pragma unroll
+            for (int i = 0; i < R::NV; ++i) {
+                const int c = R::column(i);
+                if (a.group) {
+                    float m = 0.0f;
+                    if constexpr (VE == 1) {
+                        const int n = a.group / 32, at = (i * TPR + t) / 32 / n * n;
+                        for (int k = 0; k < n; ++k) m = fmaxf(m, tops[g * (TPR * E / 32) + at + k]);
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < VE; ++j) m = fmaxf(m, fabsf(f[i * VE + j]));
+                        for (int o = a.group / VE / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+                    }
+                    scale = scale_of(m * rstd);
+                    if (on && c < cols && c % a.group == 0) scales[c / a.group] = scale;
+                }
+                if (!on || c >= cols) continue;           // behind the shuffles of this access
+                const float by = 1.0f / scale;              // up to 2^126: times rstd it could leave fp32's range
+                float q[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) q[j] = j < VE ? f[i * VE + j % VE] * rstd * by : 0.0f;
+                const uint32_t lo = pack_e4m3(q[0], q[1], q[2], q[3]), hi = pack_e4m3(q[4], q[5], q[6], q[7]);
+                if (VE == 8 && vec8) *reinterpret_cast<uint2*>(y + c) = make_uint2(lo, hi);
+                else if (VE == 4 && vec8) *reinterpret_cast<uint32_t*>(y + c) = lo;
+                else {
+#pragma unroll
+                    for (int j = 0; j < VE; ++j) y[c + j] = (uint8_t)((j < 4 ? lo : hi) >> (8 * (j & 3)));
+                }
+            }
+        }
+    }
+}
+
+template <int DT, int VB, int TPR, int E, int FORM>
+__global__ void __launch_bounds__(kBackwardThreads<TPR, E>, kBackwardBlocks<TPR, E>) rms_backward_kernel(const RmsBackArgs a) {
+    using R = RowRegs<DT, VB, TPR, E>;
+    constexpr int P = E / 2, kThreads = kBackwardThreads<TPR, E>, kGroups = kThreads / TPR;
+    constexpr bool kAhead = VB == 16 && DT == kBF16 && TPR < 1024, kKeep = TPR < 1024, kFetch = !kAhead && (TPR == 1024 || (VB == 16 && TPR >= 128));
+    __shared__ float buf[2][32];
+    extern __shared__ float fold[];                       // kGroups > 1: [cols]
+    const PhiloxKey key(a.drop.seed, a.drop.offset, FORM == kDrop ? a.drop.offset_dev : nullptr);
+    const int g = threadIdx.x / TPR, cols = (int)a.cols;
+    const float inv_n = 1.0f / (float)a.cols;
+    const long long step = (long long)gridDim.x * kGroups;
+    float2 w[P], dw[P];
+    if constexpr (kKeep) R::params(a.weight, a.weight_f32, a.weight_vec, cols, w, 1.0f);
+#pragma unroll
+    for (int k = 0; k < P; ++k) dw[k] = make_float2(0.0f, 0.0f);
+    int turn = 0;
+    typename R::Raw ud[R::NV], ux[R::NV], ue[R::NV];
+    float next_rstd = 0.0f;
+    const auto ask = [&](long long r) {
+        if constexpr (kAhead) {
+            const bool on = r < a.rows;
+            R::ask(row_of<DT>(a.dy, a.ld_dy, r), on ? cols : 0, ud);
+            R::ask(row_of<DT>(a.h, a.ld_h, r), on ? cols : 0, ux);
+            R::ask(row_of<DT>(a.dsum, a.ld_dsum, r), on && a.dsum ? cols : 0, ue);
+            next_rstd = on ? a.rstd[r] : 0.0f;
+        }
+    };
+    ask((long long)blockIdx.x * kGroups + g);
+    for (long long r0 = (long long)blockIdx.x * kGroups; r0 < a.rows; r0 += step, turn ^= 1) {
+        const long long r = r0 + g;
+        const bool on = r < a.rows;
+        constexpr bool kLate = TPR == 1024;               // dsum is read behind the reduction
+        float2 d[P], x[P], e[kLate ? 1 : P];
+        float rstd;
+        if constexpr (kAhead) {
+            R::take(ud, d);
+            R::take(ux, x);
+            if constexpr (!kLate) R::take(ue, e);         // zeros without a dsum
+            rstd = next_rstd;
+        } else {
+            R::load(row_of<DT>(a.dy, a.ld_dy, r), on ? cols : 0, d);
+            R::load(row_of<DT>(a.h, a.ld_h, r), on ? cols : 0, x);
+            rstd = on ? a.rstd[r] : 0.0f;
+            if constexpr (!kLate) R::load(row_of<DT>(a.dsum, a.ld_dsum, r), on && a.dsum ? cols : 0, e);
+        }
+        if constexpr (kFetch) {
+            R::fetch(a.dy, a.ld_dy, a.h, a.ld_h, r + step, a.rows, cols);
+            if constexpr (VB == 16) if (a.dsum) R::fetch(a.dsum, a.ld_dsum, a.dsum, a.ld_dsum, r + step, a.rows, cols);
+        }
+        ask(r + step);
+        const float2 rs = make_float2(rstd, rstd);
+        float2 s2 = make_float2(0.0f, 0.0f);
+#pragma unroll
+        for (int k = 0; k < P; ++k) {
+            x[k] = __fmul2_rn(x[k], rs);
+            dw[k] = __ffma2_rn(d[k], x[k], dw[k]);
+            if constexpr (kKeep) d[k] = __fmul2_rn(d[k], w[k]);
+        }
+        if constexpr (!kKeep) times_params<DT, VB, TPR, E>(a.weight, a.weight_f32, a.weight_vec, cols, d);
+#pragma unroll
+        for (int k = 0; k < P; ++k) s2 = __ffma2_rn(d[k], x[k], s2);
+        const float m2 = -row_sum<TPR, kGroups>(s2.x + s2.y, buf[turn]) * inv_n;
+        const float2 mm2 = make_float2(m2, m2);
+#pragma unroll
+        for (int k = 0; k < P; ++k) {
+            d[k] = __ffma2_rn(x[k], mm2, d[k]);
+            if constexpr (kLate) d[k] = __fmul2_rn(d[k], rs);
+            else d[k] = __ffma2_rn(d[k], rs, e[k]);
+        }
+        if constexpr (kLate) {
+            if (a.dsum) {
+                float* f = reinterpret_cast<float*>(d);
+#pragma unroll
+                for (int i = 0; i < R::NV; ++i)
+                    if (on && R::column(i) < cols) {
+                        float v[R::VE];
+                        R::A::load(reinterpret_cast<const char*>(row_of<DT>(a.dsum, a.ld_dsum, r) + R::column(i)), v);
+#pragma unroll
+                        for (int j = 0; j < R::VE; ++j) f[i * R::VE + j] += v[j];
+                    }
+            }
+        }
+        if (on && a.dh) R::store(row_of<DT>(a.dh, a.ld_dh, r), cols, d);
+        if constexpr (FORM == kDrop) drop_row<DT, VB, TPR, E>(key, a.drop, r, d);
+        if (on && a.dx) R::store(row_of<DT>(a.dx, a.ld_dx, r), cols, d);
+    }
+    if (!a.partials) return;
+    float* out = a.partials + (long long)blockIdx.x * a.cols;
+    const float* fw = reinterpret_cast<const float*>(dw);
+    // the groups add their columns one after the other
+#pragma unroll 1
+    for (int k = 0; k < kGroups; ++k) {
+        if (kGroups > 1) __syncthreads();
+        if (g != k) continue;
+        float* to = k + 1 == kGroups ? out : fold;
+#pragma unroll
+        for (int q = 0; q < E; ++q) {
+            const int c = R::column(q / R::VE) + q % R::VE;
+            if (c < cols) to[c] = fw[q] + (k ? fold[c] : 0.0f);
+        }
     }
 }
 
@@ -228,12 +578,13 @@ template <int DT> __global__ void __launch_bounds__(128) wide_rms_columns_kernel
     a.partials[(long long)blockIdx.y * a.cols + c] = dw;
 }
 
-// Adds up `n` partial rows: 32 columns a block, 16 warps share the rows, always in the same order
-constexpr int kFoldWarps = 16;
+// Adds up `n` partial rows: 32 columns a block, its warps share the rows, always in the same order
+constexpr int kFoldWarps = 32;
 __global__ void __launch_bounds__(32 * kFoldWarps) rms_fold_kernel(const float* partials, int n, long long cols, void* dweight, int weight_f32) {
-    __shared__ float s[kFoldWarps][32];
+    __shared__ float s[kFoldWarps][33];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const long long c = (long long)blockIdx.x * 32 + lane;
+    cudaGridDependencySynchronize();
     float v = 0.0f;
     if (c < cols)
 #pragma unroll 8
@@ -250,17 +601,73 @@ __global__ void __launch_bounds__(32 * kFoldWarps) rms_fold_kernel(const float* 
 // Rows that start on 16-byte boundaries, all of them
 bool aligned(const void* p, long long ld, int elem) { return !p || ((uintptr_t)p % 16 == 0 && (ld * elem) % 16 == 0); }
 
+constexpr long long kRegisterWidth = 16384;
+
+template <int DT, int VB, int TPR, int E, int FORM> cudaError_t forward(const RmsArgs& a, int sms, cudaStream_t stream) {
+    constexpr int kThreads = kForwardThreads<TPR>, kGroups = kThreads / TPR;
+    const long long want = (a.rows + kGroups - 1) / kGroups, cap = (long long)kForwardBlocks<TPR, E> * sms;
+    const int bytes = VB / RowType<DT>::kBytes;           // that a thread stores of y8 at a time
+    rms_forward_kernel<DT, VB, TPR, E, FORM><<<(unsigned)std::min(want, cap), kThreads, 0, stream>>>(a, (uintptr_t)a.y % bytes == 0 && a.ld_y % bytes == 0);
+    return cudaGetLastError();
+}
+template <int DT, int VB, int TPR, int E, int FORM> cudaError_t backward(const RmsBackArgs& a, int sms, int* used, cudaStream_t stream) {
+    constexpr int kThreads = kBackwardThreads<TPR, E>, kGroups = kThreads / TPR;
+    const long long want = (a.rows + kGroups - 1) / kGroups, cap = std::min<long long>((long long)kBackwardBlocks<TPR, E> * sms, rms_partial_rows(a.rows, a.cols));
+    *used = (int)std::min(want, cap);
+    const size_t smem = kGroups > 1 && a.partials ? sizeof(float) * (size_t)a.cols : 0;          // at most 8 KB: these rows have 2048 columns or fewer
+    rms_backward_kernel<DT, VB, TPR, E, FORM><<<(unsigned)*used, kThreads, smem, stream>>>(a);
+    return cudaGetLastError();
+}
+
+// The form for a row of `cols` elements: threads that share it, elements of each
+template <int DT, int VB, int FORM> cudaError_t forward_by_width(const RmsArgs& a, int sms, cudaStream_t stream) {
+    if (a.cols <= 256) return forward<DT, VB, 32, 8, FORM>(a, sms, stream);
+    if (a.cols <= 512) return forward<DT, VB, 32, 16, FORM>(a, sms, stream);
+    if (a.cols <= 1024) return forward<DT, VB, VB == 16 ? 128 : 64, VB == 16 ? 8 : 16, FORM>(a, sms, stream);
+    if (a.cols <= 2048) return forward<DT, VB, 128, 16, FORM>(a, sms, stream);
+    if (a.cols <= 4096) return forward<DT, VB, 256, 16, FORM>(a, sms, stream);
+    constexpr bool kWords = VB == 16 && DT == kF32;
+    if (a.cols <= 8192) return forward<DT, VB, kWords ? 1024 : 512, kWords ? 8 : 16, FORM>(a, sms, stream);
+    return forward<DT, VB, 1024, 16, FORM>(a, sms, stream);
+}
+template <int DT, int VB, int FORM> cudaError_t backward_by_width(const RmsBackArgs& a, int sms, int* used, cudaStream_t stream) {
+    if (a.cols <= 256) return backward<DT, VB, 32, 8, FORM>(a, sms, used, stream);
+    if (a.cols <= 512) return backward<DT, VB, 64, 8, FORM>(a, sms, used, stream);
+    if (a.cols <= 1024) return backward<DT, VB, 128, 8, FORM>(a, sms, used, stream);
+    if (a.cols <= 2048) return backward<DT, VB, 256, 8, FORM>(a, sms, used, stream);
+    if (a.cols <= 4096) return backward<DT, VB, 256, 16, FORM>(a, sms, used, stream);
+    if (a.cols <= 8192) return backward<DT, VB, VB == 16 ? 512 : 1024, VB == 16 ? 16 : 8, FORM>(a, sms, used, stream);
+    return backward<DT, VB, 1024, 16, FORM>(a, sms, used, stream);
+}
+template <int DT, int VB> cudaError_t forward_by_form(const RmsArgs& a, int sms, cudaStream_t stream) {
+    return a.scales ? forward_by_width<DT, VB, kE4m3>(a, sms, stream) : a.drop.limit ? forward_by_width<DT, VB, kDrop>(a, sms, stream)
+                                                                                     : forward_by_width<DT, VB, kPlain>(a, sms, stream);
+}
+template <int DT, int VB> cudaError_t backward_by_form(const RmsBackArgs& a, int sms, int* used, cudaStream_t stream) {
+    return a.drop.limit && a.dx ? backward_by_width<DT, VB, kDrop>(a, sms, used, stream) : backward_by_width<DT, VB, kPlain>(a, sms, used, stream);
+}
+
+template <int DT> cudaError_t dropout(const DropoutArgs& a, bool vec, int sms, cudaStream_t stream) {
+    const long long blocks = (a.cols + 7) / 8;
+    if (vec && a.cols <= 1 << 30 && a.rows <= (1ll << 30) / blocks) {          // counted in 31 bits, a stride beyond the last included
+        const uint32_t all = (uint32_t)(a.rows * blocks);
+        const unsigned grid = (unsigned)std::min<long long>((all + kDropThreads - 1) / kDropThreads, (long long)kDropBlocks * sms);
+        if (a.drop.limit) dropout_kernel<DT, true><<<grid, kDropThreads, 0, stream>>>(a, Divide((uint32_t)blocks), all);
+        else dropout_kernel<DT, false><<<grid, kDropThreads, 0, stream>>>(a, Divide((uint32_t)blocks), all);
+    } else {
+        const long long all = (a.cols + 255) / 256 * a.rows;
+        dropout_any_kernel<DT><<<(unsigned)std::min<long long>((all + kDropThreads / 32 - 1) / (kDropThreads / 32), 6ll * sms), kDropThreads, 0, stream>>>(a);
+    }
+    return cudaGetLastError();
+}
+
 }  // namespace
 
 cudaError_t launch_dropout(const DropoutArgs& a, int dtype, int sms, cudaStream_t stream) {
     if (a.rows == 0 || a.cols == 0) return cudaSuccess;
     const int e = dtype == kF32 ? 4 : 2;
-    const bool vec = aligned(a.x, a.ld_x, e) && aligned(a.residual, a.ld_residual, e) && aligned(a.y, a.ld_y, e);
-    const long long all = a.rows * ((a.cols + 7) / 8);
-    const unsigned grid = (unsigned)std::min<long long>((all + 255) / 256, 8ll * sms);
-    if (dtype == kF32) { if (vec) dropout_kernel<kF32, true><<<grid, 256, 0, stream>>>(a); else dropout_kernel<kF32, false><<<grid, 256, 0, stream>>>(a); }
-    else { if (vec) dropout_kernel<kBF16, true><<<grid, 256, 0, stream>>>(a); else dropout_kernel<kBF16, false><<<grid, 256, 0, stream>>>(a); }
-    return cudaGetLastError();
+    const bool vec = a.cols * e % 16 == 0 && aligned(a.x, a.ld_x, e) && aligned(a.residual, a.ld_residual, e) && aligned(a.y, a.ld_y, e);
+    return dtype == kF32 ? dropout<kF32>(a, vec, sms, stream) : dropout<kBF16>(a, vec, sms, stream);
 }
 
 cudaError_t launch_rms_forward(RmsArgs a, int dtype, int sms, cudaStream_t stream) {
@@ -269,6 +676,11 @@ cudaError_t launch_rms_forward(RmsArgs a, int dtype, int sms, cudaStream_t strea
     a.weight_vec = (uintptr_t)a.weight % 16 == 0;
     const bool e8 = a.scales != nullptr;
     const bool vec = aligned(a.x, a.ld_x, e) && aligned(a.residual, a.ld_residual, e) && aligned(a.sum, a.ld_sum, e) && (e8 || aligned(a.y, a.ld_y, e));
+    if (a.cols <= kRegisterWidth) {
+        const bool all = vec && a.cols * e % 16 == 0;
+        if (dtype == kF32) return all ? forward_by_form<kF32, 16>(a, sms, stream) : forward_by_form<kF32, 4>(a, sms, stream);
+        return all ? forward_by_form<kBF16, 16>(a, sms, stream) : forward_by_form<kBF16, 2>(a, sms, stream);
+    }
     const bool vec8 = (uintptr_t)a.y % 8 == 0 && a.ld_y % 8 == 0;
     const unsigned grid = (unsigned)std::min<long long>(a.rows, 4ll * sms);
     auto go = [&](auto kernel) { kernel<<<grid, kWide, 0, stream>>>(a, vec8); return cudaGetLastError(); };
@@ -286,9 +698,13 @@ cudaError_t launch_rms_backward(RmsBackArgs a, int dtype, void* dweight, int sms
     const int e = dtype == kF32 ? 4 : 2;
     a.weight_vec = (uintptr_t)a.weight % 16 == 0;
     int used = 0;
-    if (a.rows > 0) {
-        const bool vec = aligned(a.dy, a.ld_dy, e) && aligned(a.h, a.ld_h, e) && aligned(a.dsum, a.ld_dsum, e) && aligned(a.dh, a.ld_dh, e) && aligned(a.dx, a.ld_dx, e);
-        cudaError_t err;
+    cudaError_t err = cudaSuccess;
+    const bool vec = aligned(a.dy, a.ld_dy, e) && aligned(a.h, a.ld_h, e) && aligned(a.dsum, a.ld_dsum, e) && aligned(a.dh, a.ld_dh, e) && aligned(a.dx, a.ld_dx, e);
+    if (a.rows > 0 && a.cols <= kRegisterWidth) {
+        const bool all = vec && a.cols * e % 16 == 0;
+        if (dtype == kF32) err = all ? backward_by_form<kF32, 16>(a, sms, &used, stream) : backward_by_form<kF32, 4>(a, sms, &used, stream);
+        else err = all ? backward_by_form<kBF16, 16>(a, sms, &used, stream) : backward_by_form<kBF16, 2>(a, sms, &used, stream);
+    } else if (a.rows > 0) {
         if (a.partials) {
             used = rms_partial_rows(a.rows, a.cols);
             const dim3 grid((unsigned)((a.cols + 127) / 128), (unsigned)used);
@@ -300,12 +716,19 @@ cudaError_t launch_rms_backward(RmsBackArgs a, int dtype, void* dweight, int sms
         auto go = [&](auto kernel) { kernel<<<grid, kWide, 0, stream>>>(a); return cudaGetLastError(); };
         if (dtype == kF32) err = vec ? go(wide_rms_backward_kernel<kF32, true>) : go(wide_rms_backward_kernel<kF32, false>);
         else err = vec ? go(wide_rms_backward_kernel<kBF16, true>) : go(wide_rms_backward_kernel<kBF16, false>);
-        if (err != cudaSuccess) return err;
     }
-    if (!dweight) return cudaSuccess;
+    if (err != cudaSuccess || !dweight) return err;
     // rows == 0: nothing was launched and the sum over no rows is zeros (used == 0)
-    rms_fold_kernel<<<(unsigned)((a.cols + 31) / 32), 32 * kFoldWarps, 0, stream>>>(a.partials, used, a.cols, dweight, a.weight_f32);
-    return cudaGetLastError();
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)((a.cols + 31) / 32));
+    cfg.blockDim = dim3(32 * kFoldWarps);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, rms_fold_kernel, (const float*)a.partials, used, a.cols, dweight, (int)a.weight_f32);
 }
 
 }  // namespace tmask
