@@ -380,7 +380,9 @@ int tm_rms_norm_backward(const void* dy, int64_t ld_dy, const void* h, int64_t l
  * 2^31 + i / 4.  With drafted 0 a call draws one token a row from softmax(logits / temperature).
  * -Inf (a masked logit) has probability 0.  A row that is reached and holds NaN, +Inf or nothing but -Inf ends its sequence with
  * token -1 and logp NaN and raises TM_DEV_NONFINITE in *status_dev (may be NULL); an id that is not below vocab ends the drafts like a negative
- * one and raises TM_DEV_BADID.  Rows behind the first refused draft are not read.  1 <= vocab <= TM_VOCAB_MAX, 0 <= drafted <= TM_DRAFT_MAX.
+ * one and raises TM_DEV_BADID.  Rows behind the first refused draft have no part in the answer (they may be read).  The sums of a row are fp32 sums
+ * joined in fp64: p and q hold them to some 2^-23, so p - q counts as 0 where log2 p - log2 q is 2^-20 or less; comparisons that fp32 cannot tell
+ * are made in fp64.  Tokens below 2^-126 of the row's largest p are not drawn.  1 <= vocab <= TM_VOCAB_MAX, 0 <= drafted <= TM_DRAFT_MAX.
  */
 #define TM_DRAFT_MAX 1024
 int tm_verify_draft(const void* logits, int dtype, int64_t batch, int64_t drafted, int64_t vocab, int64_t ld, const void* draft_logits,

@@ -60,7 +60,8 @@ bool make_drop(double p, uint64_t seed, uint64_t offset, const uint64_t* offset_
     if (!(p >= 0.0 && p < 1.0)) return false;
     d->limit = (uint32_t)std::min(65535ll, std::llrint(p * 65536.0));
     d->scale = 65536.0f / (float)(65536u - d->limit);
-    d->seed = seed; d->offset = offset;
+    d->keys.set(seed);
+    d->offset = offset;
     d->offset_dev = reinterpret_cast<const unsigned long long*>(offset_dev);
     return true;
 }
@@ -280,7 +281,8 @@ int tm_verify_draft(const void* logits, int dtype, int64_t batch, int64_t drafte
     if (rc != TM_OK) return rc;
     tmask::VerifyArgs a = {};
     a.logits = logits; a.draft_logits = draft_logits; a.vocab = vocab; a.ld = ld; a.ld_draft = ld_draft; a.batch = (int)batch; a.drafted = (int)drafted;
-    a.ids = draft_ids; a.temperature = temperature; a.draft_temperature = draft_temperature; a.seed = seed; a.offset = offset;
+    a.ids = draft_ids; a.temperature = temperature; a.draft_temperature = draft_temperature; a.offset = offset;
+    a.keys.set(seed);
     a.offset_dev = reinterpret_cast<const unsigned long long*>(offset_dev);
     a.tokens = tokens_out; a.accepted = accepted_out; a.logp = logp_out; a.status = status_dev;
     return finish(tmask::launch_verify(a, dtype, sms, static_cast<cudaStream_t>(cuda_stream)));

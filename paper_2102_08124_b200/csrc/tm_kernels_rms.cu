@@ -62,7 +62,7 @@ __device__ __forceinline__ void load_weights(const void* w, bool f32, bool vec, 
         }
     }
 }
-__device__ __forceinline__ void drop_block(const PhiloxKey& key, const DropSpec& d, long long r, long long c, float (&v)[8]) {
+__device__ __forceinline__ void drop_block(const Philox& key, const DropSpec& d, long long r, long long c, float (&v)[8]) {
     const uint32_t kept = kept_bits(key((uint32_t)(c >> 3), (uint32_t)r), d.limit);
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = (kept >> j) & 1u ? v[j] * d.scale : 0.0f;      // a dropped Inf or NaN is gone
@@ -105,7 +105,7 @@ struct Divide {
 constexpr int kDropThreads = 256, kDropBlocks = 5;
 template <int DT, bool DROP> __global__ void __launch_bounds__(kDropThreads, kDropBlocks) dropout_kernel(const DropoutArgs a, const Divide by, uint32_t all) {
     constexpr int kEach = DT == kBF16 ? 2 : 1, V = RowType<DT>::kVec, N = 8 / V;
-    const PhiloxKey key(a.drop.seed, a.drop.offset, a.drop.offset_dev);
+    const Philox key(a.drop.keys, a.drop.offset, a.drop.offset_dev);
     const uint32_t step = gridDim.x * kDropThreads, high = a.drop.limit << 16;
     const int cols = (int)min(a.cols, (long long)INT32_MAX);
     for (uint32_t i0 = blockIdx.x * kDropThreads + threadIdx.x; i0 < all; i0 += kEach * step) {
@@ -152,7 +152,7 @@ template <int DT, bool DROP> __global__ void __launch_bounds__(kDropThreads, kDr
 // works out which columns of block k stay; a column's bit comes from there.
 template <int DT> __global__ void __launch_bounds__(kDropThreads) dropout_any_kernel(const DropoutArgs a) {
     using T = typename RowType<DT>::T;
-    const PhiloxKey key(a.drop.seed, a.drop.offset, a.drop.offset_dev);
+    const Philox key(a.drop.keys, a.drop.offset, a.drop.offset_dev);
     const long long parts = (a.cols + 255) / 256, all = a.rows * parts, step = (long long)gridDim.x * (kDropThreads / 32);
     const int lane = threadIdx.x & 31;
     for (long long i = (long long)blockIdx.x * (kDropThreads / 32) + (threadIdx.x >> 5); i < all; i += step) {
@@ -181,7 +181,7 @@ constexpr int kPlain = 0, kDrop = 1, kE4m3 = 2;      // forms of the kernels bel
 
 // Dropout of what TPR >= 32 threads hold of a row (RowRegs).  A warp's lanes work out one block of eight columns each; accesses
 // narrower than a block take their columns' bits from the lane that has them.
-template <int DT, int VB, int TPR, int E> __device__ __forceinline__ void drop_row(const PhiloxKey& key, const DropSpec& d, long long r, float2 (&v)[E / 2]) {
+template <int DT, int VB, int TPR, int E> __device__ __forceinline__ void drop_row(const Philox& key, const DropSpec& d, long long r, float2 (&v)[E / 2]) {
     constexpr int VE = Access<DT, VB>::kElems, A = 8 / VE, B = 4 * VE;      // accesses and, in each of them, blocks that a warp's 32 blocks are
     float* f = reinterpret_cast<float*>(v);
     const int t = threadIdx.x % TPR, lane = threadIdx.x & 31;
@@ -250,7 +250,7 @@ __global__ void __launch_bounds__(kForwardThreads<TPR>, kForwardBlocks<TPR, E>) 
     constexpr bool kAhead = VB == 16 ? DT == kBF16 || R::NV <= 2 : E == 16 && (TPR == 256 || TPR == 512), kKeep = TPR < 1024 || E < 16, kFetch = !kAhead && TPR >= 128;
     __shared__ float2 buf[2][32];
     __shared__ float tops[FORM == kE4m3 && VE == 1 ? kGroups * TPR * E / 32 : 1];
-    const PhiloxKey key(a.drop.seed, a.drop.offset, FORM == kDrop ? a.drop.offset_dev : nullptr);
+    const Philox key(a.drop.keys, a.drop.offset, FORM == kDrop ? a.drop.offset_dev : nullptr);
     const int t = threadIdx.x % TPR, g = threadIdx.x / TPR, cols = (int)a.cols, lane = threadIdx.x & 31;
     const float inv_n = 1.0f / (float)a.cols;
     const long long step = (long long)gridDim.x * kGroups;
@@ -361,7 +361,7 @@ __global__ void __launch_bounds__(kBackwardThreads<TPR, E>, kBackwardBlocks<TPR,
     constexpr bool kAhead = VB == 16 && DT == kBF16 && TPR < 1024, kKeep = TPR < 1024, kFetch = !kAhead && (TPR == 1024 || (VB == 16 && TPR >= 128));
     __shared__ float buf[2][32];
     extern __shared__ float fold[];                       // kGroups > 1: [cols]
-    const PhiloxKey key(a.drop.seed, a.drop.offset, FORM == kDrop ? a.drop.offset_dev : nullptr);
+    const Philox key(a.drop.keys, a.drop.offset, FORM == kDrop ? a.drop.offset_dev : nullptr);
     const int g = threadIdx.x / TPR, cols = (int)a.cols;
     const float inv_n = 1.0f / (float)a.cols;
     const long long step = (long long)gridDim.x * kGroups;
@@ -461,7 +461,7 @@ __global__ void __launch_bounds__(kBackwardThreads<TPR, E>, kBackwardBlocks<TPR,
 constexpr int kWide = 512;
 template <int DT, bool VEC, bool E8> __global__ void __launch_bounds__(kWide) wide_rms_forward_kernel(const RmsArgs a, bool vec8) {
     __shared__ float2 buf[2][32];
-    const PhiloxKey key(a.drop.seed, a.drop.offset, a.drop.offset_dev);
+    const Philox key(a.drop.keys, a.drop.offset, a.drop.offset_dev);
     const float inv_n = 1.0f / (float)a.cols;
     const int lane = threadIdx.x & 31;
     const long long blocks = (a.cols + 7) / 8;
@@ -533,7 +533,7 @@ template <int DT, bool VEC, bool E8> __global__ void __launch_bounds__(kWide) wi
 
 template <int DT, bool VEC> __global__ void __launch_bounds__(kWide) wide_rms_backward_kernel(const RmsBackArgs a) {
     __shared__ float buf[2][32];
-    const PhiloxKey key(a.drop.seed, a.drop.offset, a.drop.offset_dev);
+    const Philox key(a.drop.keys, a.drop.offset, a.drop.offset_dev);
     const float inv_n = 1.0f / (float)a.cols;
     const long long blocks = (a.cols + 7) / 8;
     int turn = 0;

@@ -142,11 +142,20 @@ struct DistillArgs {                            // tm_kernels_distill.cu
 };
 cudaError_t launch_distill(const DistillArgs& a, int dtype, bool loss, bool grad, int sms, cudaStream_t stream);
 
+// Keys of the counter-based generator's rounds (tm_philox.cuh)
+constexpr int kPhiloxRounds = 10;
+struct PhiloxKeys {
+    uint32_t k[2 * kPhiloxRounds];
+    void set(uint64_t seed) {
+        for (uint32_t i = 0; i < kPhiloxRounds; ++i) { k[2 * i] = (uint32_t)seed + i * 0x9E3779B9u; k[2 * i + 1] = (uint32_t)(seed >> 32) + i * 0xBB67AE85u; }
+    }
+};
 // Dropout from the counter-based generator of tm_philox.cuh: an element stays where its 16 bits are `limit` or more (0: there is none), times `scale`.
 struct DropSpec {
     uint32_t limit;
     float scale;                                // 65536 / (65536 - limit)
-    unsigned long long seed, offset;
+    PhiloxKeys keys;
+    unsigned long long offset;
     const unsigned long long* offset_dev;       // or null; added to offset
 };
 // The residual branch (tm_kernels_rms.cu)
@@ -188,7 +197,8 @@ struct VerifyArgs {                             // tm_kernels_verify.cu
     int batch, drafted;
     const int* ids;
     float temperature, draft_temperature;
-    unsigned long long seed, offset;
+    PhiloxKeys keys;
+    unsigned long long offset;
     const unsigned long long* offset_dev;       // or null
     int *tokens, *accepted;
     float* logp;                                // or null

@@ -8,22 +8,22 @@
 
 namespace tmask {
 
-// What a kernel works with: the seed's halves and the offset's
-struct PhiloxKey {
-    uint32_t k0, k1, o0, o1;
-    __device__ __forceinline__ PhiloxKey(unsigned long long seed, unsigned long long offset, const unsigned long long* offset_dev) {
+// A kernel's generator: the keys of the rounds lie among its arguments, so that they are operands and no instructions
+struct Philox {
+    const PhiloxKeys& keys;
+    uint32_t o0, o1;
+    __device__ __forceinline__ Philox(const PhiloxKeys& keys_, unsigned long long offset, const unsigned long long* offset_dev) : keys(keys_) {
         if (offset_dev) offset += *offset_dev;
-        k0 = (uint32_t)seed; k1 = (uint32_t)(seed >> 32);
         o0 = (uint32_t)offset; o1 = (uint32_t)(offset >> 32);
     }
     __device__ __forceinline__ uint4 operator()(uint32_t block, uint32_t row) const {
         uint32_t c0 = block, c1 = row, c2 = o0, c3 = o1;
 #pragma unroll
-        for (uint32_t i = 0; i < 10; ++i) {
+        for (int i = 0; i < kPhiloxRounds; ++i) {
             const unsigned long long a = (unsigned long long)c0 * 0xD2511F53u, b = (unsigned long long)c2 * 0xCD9E8D57u;
-            c0 = (uint32_t)(b >> 32) ^ c1 ^ (k0 + i * 0x9E3779B9u);
+            c0 = (uint32_t)(b >> 32) ^ c1 ^ keys.k[2 * i];
             c1 = (uint32_t)b;
-            c2 = (uint32_t)(a >> 32) ^ c3 ^ (k1 + i * 0xBB67AE85u);
+            c2 = (uint32_t)(a >> 32) ^ c3 ^ keys.k[2 * i + 1];
             c3 = (uint32_t)a;
         }
         return make_uint4(c0, c1, c2, c3);

@@ -127,7 +127,8 @@ def verify(target, draft, ids, seed, offset, t, td):
                 r = p
             key = r / noise[b]
             x = int(key.argmax())
-            key[x], best = 0.0, key[x]
+            best = key[x]
+            key[x] = 0.0
             sure[b] &= key.max() < best * (1 - (close if r is p else 2.0 ** -8))
             tokens[b, n], logps[b, n] = x, logp[x]
             break

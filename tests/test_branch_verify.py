@@ -205,3 +205,10 @@ def test_what_comes_out_is_distributed_as_the_target(certain):
     bonus = tokens[:, 1][accepted == 1].cpu().long()
     m = bonus.numel()
     assert bool(((torch.bincount(bonus, minlength=vocab).double() - m * p).abs() <= 6 * (m * p * (1 - p)).sqrt()).all())
+
+
+@pytest.mark.parametrize("kind", ["drafter", "certain", "none"])
+def test_near_keys_are_told_apart(kind):
+    """Enough sequences that a few dozen have two keys, or the two sides of a test, within 2^-11 of each other."""
+    target, draft, ids = _inputs(30000, 0 if kind == "none" else 1, 24, "f32", 40)
+    _check(target, draft if kind == "drafter" else None, ids, least=0.97)
