@@ -309,36 +309,48 @@ __global__ void __launch_bounds__(kForwardThreads<TPR>, kForwardBlocks<TPR, E>) 
         } else {
             const float* f = reinterpret_cast<const float*>(h);
             uint8_t* y = static_cast<uint8_t*>(a.y) + r * a.ld_y;
-            float* scales = a.scales + r * (a.group ? (cols + a.group - 1) / a.group : 1);
+            const int shift = __ffs(a.group) - 1;          // a.group is a power of two, or 0
+            float* scales = a.scales + r * (a.group ? (cols + a.group - 1) >> shift : 1);
             float scale = scale_of(top * rstd);
             if (a.group == 0 && t == 0 && on) scales[0] = scale;
             if (VE == 1 && a.group) {                     // a warp's accesses are 32 columns each
-                float* mine = tops + g * (TPR * E / 32);
+                constexpr int kTops = TPR * E / 32;
+                float* mine = tops + g * kTops;
 #pragma unroll
                 for (int i = 0; i < R::NV; ++i) {
                     const float m = group_max<32>(fabsf(f[i]));
                     if (lane == 0) mine[(i * TPR + t) / 32] = m;
                 }
+                row_barrier<TPR, kGroups>();
+                const int n = a.group / 32, groups = kTops >> (shift - 5);
+                float m = 0.0f;
+                if (t < groups) {
+                    for (int k = 0; k < n; ++k) m = fmaxf(m, mine[t * n + k]);
+                    scale = scale_of(m * rstd);
+                    if (on && t * a.group < cols) scales[t] = scale;
+                    m = __fdividef(1.0f, scale);
+                }
+                row_barrier<TPR, kGroups>();
+                if (t < groups) mine[t] = m;           // from here on the groups' inverses
                 row_barrier<TPR, kGroups>();               // the next row's writes come behind its reduction, which waits for these reads
             }
+            float by = __fdividef(1.0f, scale);            // up to 2^126: times rstd it could leave fp32's range
 #pragma unroll
             for (int i = 0; i < R::NV; ++i) {
                 const int c = R::column(i);
                 if (a.group) {
-                    float m = 0.0f;
-                    if constexpr (VE == 1) {
-                        const int n = a.group / 32, at = (i * TPR + t) / 32 / n * n;
-                        for (int k = 0; k < n; ++k) m = fmaxf(m, tops[g * (TPR * E / 32) + at + k]);
-                    } else {
+                    if constexpr (VE == 1) by = tops[g * (TPR * E / 32) + (c >> shift)];
+                    else {
+                        float m = 0.0f;
 #pragma unroll
                         for (int j = 0; j < VE; ++j) m = fmaxf(m, fabsf(f[i * VE + j]));
                         for (int o = a.group / VE / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+                        scale = scale_of(m * rstd);
+                        by = __fdividef(1.0f, scale);
+                        if (on && c < cols && (c & (a.group - 1)) == 0) scales[c >> shift] = scale;
                     }
-                    scale = scale_of(m * rstd);
-                    if (on && c < cols && c % a.group == 0) scales[c / a.group] = scale;
                 }
                 if (!on || c >= cols) continue;           // behind the shuffles of this access
-                const float by = 1.0f / scale;              // up to 2^126: times rstd it could leave fp32's range
                 float q[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) q[j] = j < VE ? f[i * VE + j % VE] * rstd * by : 0.0f;
@@ -358,7 +370,7 @@ template <int DT, int VB, int TPR, int E, int FORM>
 __global__ void __launch_bounds__(kBackwardThreads<TPR, E>, kBackwardBlocks<TPR, E>) rms_backward_kernel(const RmsBackArgs a) {
     using R = RowRegs<DT, VB, TPR, E>;
     constexpr int P = E / 2, kThreads = kBackwardThreads<TPR, E>, kGroups = kThreads / TPR;
-    constexpr bool kAhead = VB == 16 && DT == kBF16 && TPR < 1024, kKeep = TPR < 1024, kFetch = !kAhead && (TPR == 1024 || (VB == 16 && TPR >= 128));
+    constexpr bool kAhead = VB == 16 && DT == kBF16 && TPR < 1024, kKeep = TPR < 1024 || E == 8, kFetch = !kAhead && (TPR == 1024 || (VB == 16 && TPR >= 128));
     __shared__ float buf[2][32];
     extern __shared__ float fold[];                       // kGroups > 1: [cols]
     const Philox key(a.drop.keys, a.drop.offset, FORM == kDrop ? a.drop.offset_dev : nullptr);
