@@ -12,6 +12,7 @@ from typing import NamedTuple, Optional
 
 from . import binding as tm
 from . import binding_train as tt
+from .branch import _rows, dropout, rms_norm
 from .refresh import MaskRefresher, masked_linear
 
 _functions = None
@@ -28,13 +29,6 @@ class TeacherLists(NamedTuple):
 def teacher_lists(logits, k: int, temperature: float = 1.0, status=None) -> TeacherLists:
     values, ids, lse = tt.tm_top_logits(logits.detach(), k, temperature, status=status)
     return TeacherLists(values, ids, lse, temperature)
-
-
-def _rows(t):
-    """As a matrix whose rows lie apart from each other, copied if need be (the gradient of a sum is an expanded scalar or row)."""
-    t = t.reshape(-1, t.shape[-1])
-    apart = (t.shape[1] <= 1 or t.stride(1) == 1) and (t.shape[0] <= 1 or t.stride(0) >= t.shape[1])
-    return t if apart else t.contiguous()
 
 
 def _make():
@@ -122,10 +116,14 @@ def distill_backward(logits, teacher: TeacherLists, row_weight=None, scale: floa
 
 
 class Blocks:
-    """A small pre-norm network over token ids: embedding, blocks of norm, wide linear, gelu, linear, and a norm before the output layer."""
+    """A small pre-norm network over token ids: embedding, blocks of norm, wide linear, gelu, linear, and a norm before the output layer.
+    norm: "layer", or "rms" (without the biases)."""
 
-    def __init__(self, vocab: int, width: int, blocks: int, dtype, device, seed: int = 0):
+    def __init__(self, vocab: int, width: int, blocks: int, dtype, device, seed: int = 0, norm: str = "layer"):
         import torch
+        if norm not in ("layer", "rms"):
+            raise ValueError("norm must be layer or rms")
+        self.norm = norm
         g = torch.Generator(device="cpu").manual_seed(seed)
 
         def weight(rows, cols, scale):
@@ -136,7 +134,7 @@ class Blocks:
         for _ in range(blocks):
             self.linear += [weight(4 * width, width, width ** -0.5), weight(width, 4 * width, (4 * width) ** -0.5)]
         self.norm_weight = [torch.ones(width, dtype=dtype, device=device) for _ in range(blocks + 1)]
-        self.norm_bias = [torch.zeros(width, dtype=dtype, device=device) for _ in range(blocks + 1)]
+        self.norm_bias = [torch.zeros(width, dtype=dtype, device=device) for _ in range(blocks + 1)] if norm == "layer" else []
         self.head = weight(vocab, width, 2.0 * width ** -0.5)
 
     def parameters(self):
@@ -144,32 +142,45 @@ class Blocks:
 
     def copy(self) -> "Blocks":
         other = object.__new__(Blocks)
+        other.norm = self.norm
         other.embedding, other.head = self.embedding, self.head          # shared, not trained
         for name in ("linear", "norm_weight", "norm_bias"):
             setattr(other, name, [p.detach().clone().requires_grad_() for p in getattr(self, name)])
         return other
 
-    def logits(self, tokens, masked: Optional[list] = None):
-        """masked: the linear layers' masked weights; None runs the dense ones."""
+    def _norm(self, i, update, h, p, seed, offset):
+        """Norm i of h + dropout(update): (y, the sum)."""
+        if self.norm == "rms":
+            return rms_norm(h if update is None else update, self.norm_weight[i], residual=None if update is None else h, p=0.0 if update is None else p,
+                            seed=seed, offset=offset + i)
+        if update is not None and p > 0:
+            h, update = dropout(update, p, seed, offset + i, residual=h), None
+        return layer_norm(h if update is None else update, self.norm_weight[i], self.norm_bias[i], residual=None if update is None else h)
+
+    def logits(self, tokens, masked: Optional[list] = None, p: float = 0.0, seed: int = 0, offset: int = 0):
+        """masked: the linear layers' masked weights; None runs the dense ones.  p: dropout of the blocks' outputs, from seed and as many offsets as
+        there are norms."""
         import torch
         h, update = self.embedding[tokens], None
         for i in range(len(self.linear) // 2):
-            y, h = layer_norm(h if update is None else update, self.norm_weight[i], self.norm_bias[i], residual=None if update is None else h)
+            y, h = self._norm(i, update, h, p, seed, offset)
             a, b = self.linear[2 * i], self.linear[2 * i + 1]
             if masked is None:
                 update = torch.nn.functional.gelu(y @ a.t()) @ b.t()
             else:
                 update = masked_linear(torch.nn.functional.gelu(masked_linear(y, a, masked[2 * i])), b, masked[2 * i + 1])
-        y, _ = layer_norm(update, self.norm_weight[-1], self.norm_bias[-1], residual=h)
+        y, _ = self._norm(len(self.linear) // 2, update, h, p, seed, offset)
         return y @ self.head.t()
 
 
 def train(steps: int = 60, rows: int = 512, vocab: int = 4099, width: int = 256, blocks: int = 2, k: int = 32, temperature: float = 2.0,
-          lr: float = 1e-3, period: int = 1, dtype=None, device: str = "cuda", seed: int = 0, evaluate: int = 20, report=None):
-    """Distils a dense network into its 2:4 transposable pruning; returns the mean losses on held-out tokens, before, during and after."""
+          lr: float = 1e-3, period: int = 1, dtype=None, device: str = "cuda", seed: int = 0, evaluate: int = 20, report=None, norm: str = "layer",
+          dropout: float = 0.0, networks: Optional[list] = None):
+    """Distils a dense network into its 2:4 transposable pruning; returns the mean losses on held-out tokens, before, during and after.
+    dropout: of the student's blocks while it trains.  networks: a list that receives the teacher, the student and the student's masked weights."""
     import torch
     dtype = dtype or torch.float32
-    teacher = Blocks(vocab, width, blocks, dtype, device, seed)
+    teacher = Blocks(vocab, width, blocks, dtype, device, seed, norm)
     student = teacher.copy()
     refresher = MaskRefresher([p.detach() for p in student.linear], N=2, M=4, period=period, method=tm.TM_EXACT, use_graph=False)
     optimizer = torch.optim.Adam(student.parameters(), lr=lr)
@@ -191,13 +202,15 @@ def train(steps: int = 60, rows: int = 512, vocab: int = 4099, width: int = 256,
         with torch.no_grad():
             lists = teacher_lists(teacher.logits(tokens), k, temperature)
         optimizer.zero_grad(set_to_none=True)
-        distill_backward(student.logits(tokens, refresher.masked_weights), lists, scale=temperature ** 2 / rows)
+        distill_backward(student.logits(tokens, refresher.masked_weights, dropout, seed, i * (blocks + 1)), lists, scale=temperature ** 2 / rows)
         optimizer.step()
         refresher.step(i)
         if i % evaluate == 0 or i == steps:
             losses.append(held_out(test, test_lists))
             if report:
                 report("step %d: loss %.5f (dense weights pruned without training %.5f), %d mask bits changed" % (i, losses[-1], losses[0], refresher.changed_bits[-1]))
+    if networks is not None:
+        networks[:] = [teacher, student, refresher.masked_weights]
     return losses
 
 
@@ -211,6 +224,8 @@ def main(argv=None):
     p.add_argument("--k", type=int, default=32)
     p.add_argument("--temperature", type=float, default=2.0)
     p.add_argument("--dtype", choices=["float32", "bfloat16"], default="float32")
+    p.add_argument("--norm", choices=["layer", "rms"], default="layer")
+    p.add_argument("--dropout", type=float, default=0.0)
     a = vars(p.parse_args(argv))
     import torch
     a["dtype"] = getattr(torch, a["dtype"])
