@@ -6,6 +6,7 @@ another seed or offset.  offset_dev (int64[1] on the device, or None) is added t
 from __future__ import annotations
 
 import ctypes
+import functools
 
 from . import binding
 from . import binding_train as bt
@@ -98,7 +99,7 @@ def tm_rms_norm(x, weight=None, eps: float = 1e-5, residual=None, p: float = 0.0
     if rstd_out is not None:
         rp = bt._array(rstd_out, (rows,), _torch.float32, dev, "rstd_out")
     elif want_stats:
-        rstd_out = _torch.empty((rows,), dtype=_torch.float32, device=dev)
+        rstd_out = _torch.empty(rows, dtype=_torch.float32, device=dev)
         rp = rstd_out.data_ptr()
     bt._call(lib.tm_rms_norm, dev, x.data_ptr(), ld, bt._ptr(residual), ld_r, code, rows, cols, wp, wcode, eps, p, seed, offset, _offset(offset_dev, dev),
              bt._ptr(sum_out), ld_s, y.data_ptr(), ld_y, rp)
@@ -127,23 +128,31 @@ def tm_rms_norm_e4m3(x, weight=None, eps: float = 1e-5, residual=None, group: in
         sum_out = bt._like(x)
     e4m3, f32 = _torch.float8_e4m3fn, _torch.float32
     if y8 is None:
-        y8 = _torch.empty((rows, cols), dtype=e4m3, device=dev)
+        y8 = _torch.empty_like(x, dtype=e4m3) if x.is_contiguous() else _torch.empty(rows, cols, dtype=e4m3, device=dev)
     else:
         if y8.dtype is not e4m3:
             raise TmError(5, "y8 must be float8_e4m3fn")
         if y8.shape != x.shape or y8.device != dev or (cols > 1 and y8.stride(1) != 1 and rows > 0):
             raise TmError(2, "y8 must have the shape and device of x, and unit column stride")
         ld_y = y8.stride(0) if rows > 1 else cols
-    shape = (rows, -(-cols // group) if group else 1)
+    groups = -(-cols // group) if group else 1
     if scales_out is None:
-        scales_out = _torch.empty(shape, dtype=f32, device=dev)
+        scales_out = _torch.empty(rows, groups, dtype=f32, device=dev)
+        sp = scales_out.data_ptr()
+    else:
+        sp = bt._array(scales_out, (rows, groups), f32, dev, "scales_out")
     bt._call(lib.tm_rms_norm_e4m3, dev, x.data_ptr(), ld, bt._ptr(residual), ld_r, code, rows, cols, wp, wcode, eps, group, bt._ptr(sum_out), ld_s,
-             y8.data_ptr(), ld_y, bt._array(scales_out, shape, f32, dev, "scales_out"), bt._array(rstd_out, (rows,), f32, dev, "rstd_out"))
+             y8.data_ptr(), ld_y, sp, bt._array(rstd_out, (rows,), f32, dev, "rstd_out"))
     if cols == 0:                                           # of which the entry writes nothing
         for t in (scales_out, rstd_out):
             if t is not None:
                 t.fill_(float("nan"))
     return y8, scales_out, sum_out
+
+
+@functools.lru_cache(maxsize=64)
+def _workspace_bytes(rows, cols):
+    return _lib().tm_rms_norm_workspace_bytes(rows, cols)
 
 
 def tm_rms_norm_workspace_bytes(rows: int, cols: int) -> int:
@@ -176,12 +185,12 @@ def tm_rms_norm_backward(dy, h, rstd, weight=None, dsum=None, p: float = 0.0, se
     if dweight_out is not None:
         dwp = bt._array(dweight_out, (cols,), kind, dev, "dweight_out")
     elif want_weight:
-        dweight_out = _torch.empty((cols,), dtype=kind, device=dev)
+        dweight_out = _torch.empty(cols, dtype=kind, device=dev)
         dwp = dweight_out.data_ptr()
     if dwp is not None:
         if workspace is None:
-            bytes_ = lib.tm_rms_norm_workspace_bytes(rows, cols)
-            workspace = _torch.empty((bytes_,), dtype=_torch.uint8, device=dev)
+            bytes_ = _workspace_bytes(rows, cols)
+            workspace = _torch.empty(bytes_, dtype=_torch.uint8, device=dev)
         else:
             if workspace.device != dev or not workspace.is_contiguous():
                 raise TmError(8, "workspace must be a contiguous tensor on the matrix's device")
@@ -216,15 +225,23 @@ def tm_verify_draft(logits, draft_logits, draft_ids, seed: int, offset: int = 0,
         if vocab > 1 and drafted and batch and draft_logits.stride(1) != 1:
             raise TmError(2, "draft_logits must have unit column stride")
         ld_d = draft_logits.stride(0) if batch * drafted > 1 else vocab
+    empty, lp = _torch.empty, None
     if tokens_out is None:
-        tokens_out = _torch.empty(shape, dtype=i32, device=dev)
+        tokens_out = empty(batch, drafted + 1, dtype=i32, device=dev)
+        tp = tokens_out.data_ptr()
+    else:
+        tp = bt._array(tokens_out, shape, i32, dev, "tokens_out")
     if accepted_out is None:
-        accepted_out = _torch.empty((batch,), dtype=i32, device=dev)
-    if logp_out is None and want_logp:
-        logp_out = _torch.empty(shape, dtype=f32, device=dev)
+        accepted_out = empty(batch, dtype=i32, device=dev)
+        ap = accepted_out.data_ptr()
+    else:
+        ap = bt._array(accepted_out, (batch,), i32, dev, "accepted_out")
+    if logp_out is not None:
+        lp = bt._array(logp_out, shape, f32, dev, "logp_out")
+    elif want_logp:
+        logp_out = empty(batch, drafted + 1, dtype=f32, device=dev)
+        lp = logp_out.data_ptr()
     bt._call(lib.tm_verify_draft, dev, logits.data_ptr(), code, batch, drafted, vocab, ld, bt._ptr(draft_logits), ld_d,
              bt._array(draft_ids, (batch, drafted), i32, dev, "draft_ids"), temperature, temperature if draft_temperature is None else draft_temperature,
-             seed, offset, _offset(offset_dev, dev), bt._array(tokens_out, shape, i32, dev, "tokens_out"),
-             bt._array(accepted_out, (batch,), i32, dev, "accepted_out"), bt._array(logp_out, shape, f32, dev, "logp_out"),
-             bt._array(status, (1,), i32, dev, "status"))
+             seed, offset, _offset(offset_dev, dev), tp, ap, lp, bt._array(status, (1,), i32, dev, "status"))
     return tokens_out, accepted_out, logp_out
