@@ -179,17 +179,135 @@ template <int DT> __global__ void __launch_bounds__(kDropThreads) dropout_any_ke
 
 constexpr int kPlain = 0, kDrop = 1, kE4m3 = 2;      // forms of the kernels below
 
-// Dropout of what TPR >= 32 threads hold of a row (RowRegs).  A warp's lanes work out one block of eight columns each; accesses
-// narrower than a block take their columns' bits from the lane that has them.
-template <int DT, int VB, int TPR, int E> __device__ __forceinline__ void drop_row(const Philox& key, const DropSpec& d, long long r, float2 (&v)[E / 2]) {
-    constexpr int VE = Access<DT, VB>::kElems, A = 8 / VE, B = 4 * VE;      // accesses and, in each of them, blocks that a warp's 32 blocks are
+// How a row is accessed: VB = 16: all rows of all matrices start on 16-byte boundaries; VB = kLead: every matrix's row starts `lead` elements behind
+// such a boundary, and the threads' columns start at -lead, so that accesses are whole vectors but at the row's ends; VB = kAny: an element
+// at a time.  With kLead a group of threads keeps to rows of one lead (rows repeat it), so that its columns' weights, sums and random numbers stay its own.
+constexpr int kLead = 0;
+template <int DT> constexpr int kAny = RowType<DT>::kBytes;
+
+// A matrix that is read
+struct Of {
+    const void* p;
+    long long ld, rows;
+    template <int DT> __device__ __forceinline__ const typename RowType<DT>::T* row(long long r) const { return row_of<DT>(p, ld, r); }
+};
+
+// A vector from column c on, an element at a time: at the matrix's very first and last elements
+template <int DT> __device__ __noinline__ uint4 first_or_last(const typename RowType<DT>::T* row, int c, int cols) {
+    uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int j = 0; j < RowType<DT>::kVec; ++j) {
+        if (c + j < 0 || c + j >= cols) continue;
+        if constexpr (DT == kF32) w[j] = __float_as_uint(row[c + j]);
+        else w[j / 2] |= (uint32_t)__bfloat16_as_ushort(row[c + j]) << (16 * (j & 1));
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+template <int DT, int VB, int TPR, int E> struct Row : RowRegs<DT, VB, TPR, E> {
+    using R = RowRegs<DT, VB, TPR, E>;
+    using T = typename RowType<DT>::T;
+    using Raw = typename R::Raw;
+    static __device__ __forceinline__ int column(int i, int) { return R::column(i); }
+    static __device__ __forceinline__ void load(const Of& m, long long r, int cols, int, float2 (&v)[E / 2]) { R::load(m.row<DT>(r), cols, v); }
+    static __device__ __forceinline__ void ask(const Of& m, long long r, int cols, int, Raw (&u)[R::NV]) { R::ask(m.row<DT>(r), cols, u); }
+    static __device__ __forceinline__ void ends(const Of&, long long, int, int, Raw (&)[R::NV]) {}
+    static __device__ __forceinline__ void inside(int, int, float2 (&)[E / 2]) {}
+    static __device__ __forceinline__ void store(T* row, int cols, int, const float2 (&v)[E / 2]) { R::store(row, cols, v); }
+    static __device__ __forceinline__ void params(const void* p, bool f32, bool vec, int cols, int, float2 (&v)[E / 2]) { R::params(p, f32, vec, cols, v, 1.0f); }
+    // VE values of row from column c on
+    static __device__ __forceinline__ void some(const Of& m, long long r, int c, int, float* v) { R::A::load(reinterpret_cast<const char*>(m.row<DT>(r) + c), v); }
+    static __device__ __forceinline__ bool any(int c, int cols) { return c < cols; }
+};
+template <int DT, int TPR, int E> struct Row<DT, kLead, TPR, E> : RowRegs<DT, 16, TPR, E> {
+    using R = RowRegs<DT, 16, TPR, E>;
+    using T = typename RowType<DT>::T;
+    using Raw = uint4;
+    static constexpr int VE = R::VE, NV = R::NV;
+    static __device__ __forceinline__ int column(int i, int lead) { return R::column(i) - lead; }
+    static __device__ __forceinline__ bool any(int c, int cols) { return cols > 0 && c + VE > 0 && c < cols; }      // cols is 0 where there is no row
+    // Vectors at a row's ends reach into its neighbours (rows are a vector long at least), and are read whole; but for those that would lie before the
+    // matrix's first element or behind its last one, whose elements ends() adds
+    static __device__ __forceinline__ bool whole(long long r, long long rows, int c, int cols) {
+        return any(c, cols) && (c >= 0 || r > 0) && (c + VE <= cols || r + 1 < rows);
+    }
+    static __device__ __forceinline__ uint4 vector(const Of& m, long long r, int c, int cols) {
+        uint4 u = make_uint4(0, 0, 0, 0);
+        if (whole(r, m.rows, c, cols)) u = *reinterpret_cast<const uint4*>(m.row<DT>(r) + c);
+        return u;
+    }
+    static __device__ __forceinline__ void ends(const Of& m, long long r, int cols, int lead, uint4 (&u)[NV]) {
+        if (r > 0 && r + 1 < m.rows) return;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = column(i, lead);
+            if (any(c, cols) && !whole(r, m.rows, c, cols)) u[i] = first_or_last<DT>(m.row<DT>(r), c, cols);
+        }
+    }
+    static __device__ __forceinline__ void ask(const Of& m, long long r, int cols, int lead, uint4 (&u)[NV]) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) u[i] = vector(m, r, column(i, lead), cols);
+    }
+    static __device__ __forceinline__ void load(const Of& m, long long r, int cols, int lead, float2 (&v)[E / 2]) {
+        uint4 u[NV];
+        ask(m, r, cols, lead, u);
+        ends(m, r, cols, lead, u);
+        R::take(u, v);
+    }
+    static __device__ __forceinline__ void some(const Of& m, long long r, int c, int cols, float* v) {
+        uint4 u = vector(m, r, c, cols);
+        if (any(c, cols) && !whole(r, m.rows, c, cols)) u = first_or_last<DT>(m.row<DT>(r), c, cols);
+        unpack_vector<DT>(u, v);
+    }
+    // zeros in the place of what lies before and behind the row
+    static __device__ __forceinline__ void inside(int cols, int lead, float2 (&v)[E / 2]) {
+        float* f = reinterpret_cast<float*>(v);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = column(i, lead);
+            if (c >= 0 && c + VE <= cols) continue;
+#pragma unroll
+            for (int j = 0; j < VE; ++j) f[i * VE + j] = c + j >= 0 && c + j < cols ? f[i * VE + j] : 0.0f;
+        }
+    }
+    static __device__ __forceinline__ void store(T* row, int cols, int lead, const float2 (&v)[E / 2]) {
+        const float* f = reinterpret_cast<const float*>(v);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = column(i, lead);
+            if (c >= 0 && c + VE <= cols) R::A::store(row + c, f + i * VE);
+            else if (any(c, cols)) {
+#pragma unroll
+                for (int j = 0; j < VE; ++j) if (c + j >= 0 && c + j < cols) from_float(row + c + j, f[i * VE + j]);
+            }
+        }
+    }
+    static __device__ __forceinline__ void params(const void* p, bool f32, bool, int cols, int lead, float2 (&v)[E / 2]) {
+        float* f = reinterpret_cast<float*>(v);
+#pragma unroll
+        for (int k = 0; k < E; ++k) {
+            const int c = column(k / VE, lead) + k % VE;
+            f[k] = 0.0f;
+            if (c >= 0 && c < cols) load_params<1>(p, f32, false, c, f + k, 1.0f);
+        }
+    }
+};
+
+// Dropout of what TPR >= 32 threads hold of a row.  A warp's lanes work out one block of eight columns each; accesses that are narrower than a
+// block, or start inside one, take their columns' bits from the lanes that have them (with a lead, an access touches one block more: lane i has
+// access i's).
+template <int DT, int VB, int TPR, int E> __device__ __forceinline__ void drop_row(const Philox& key, const DropSpec& d, long long r, int lead, float2 (&v)[E / 2]) {
+    using R = Row<DT, VB, TPR, E>;
+    constexpr int VE = R::VE, NV = R::NV, A = 8 / VE, B = 4 * VE;      // accesses that a warp's 32 blocks are, and blocks of each
     float* f = reinterpret_cast<float*>(v);
     const int t = threadIdx.x % TPR, lane = threadIdx.x & 31;
+    const auto first = [&](int i) { return (i * TPR + t - lane) * VE - lead; };      // the warp's first column in access i
+    uint32_t more = 0;
+    if constexpr (VB == kLead) more = kept_bits(key((uint32_t)((first(min(lane, NV - 1)) >> 3) + B), (uint32_t)r), d.limit);
 #pragma unroll
-    for (int k = 0; k < E / 8; ++k) {
-        const uint32_t block = (uint32_t)((k * A + lane / B) * (TPR * VE / 8) + (t - lane) * VE / 8 + lane % B);
-        const uint4 w = key(block, (uint32_t)r);
-        if constexpr (VE == 8) {
+    for (int k = 0; k < NV / A; ++k) {
+        const uint4 w = key((uint32_t)((first(k * A + lane / B) >> 3) + lane % B), (uint32_t)r);
+        if constexpr (VE == 8 && VB != kLead) {
             const uint32_t high = d.limit << 16, u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
             for (int j = 0; j < 8; ++j) f[8 * k + j] = (j & 1 ? u[j / 2] : u[j / 2] << 16) >= high ? f[8 * k + j] : 0.0f;
@@ -197,7 +315,14 @@ template <int DT, int VB, int TPR, int E> __device__ __forceinline__ void drop_r
             const uint32_t kept = kept_bits(w, d.limit);
 #pragma unroll
             for (int i = 0; i < A; ++i) {
-                const uint32_t bits = __shfl_sync(0xFFFFFFFFu, kept, i * B + lane * VE / 8) >> (lane * VE & 7);
+                uint32_t bits;
+                if constexpr (VB != kLead) bits = __shfl_sync(0xFFFFFFFFu, kept, i * B + lane * VE / 8) >> (lane * VE & 7);
+                else {
+                    const int at = (first(k * A + i) & 7) + lane * VE, q = at >> 3;      // columns from the first block's start on; block
+                    const uint32_t lo = __shfl_sync(0xFFFFFFFFu, kept, i * B + min(q, B - 1)), hi = __shfl_sync(0xFFFFFFFFu, kept, i * B + min(q + 1, B - 1));
+                    const uint32_t past = __shfl_sync(0xFFFFFFFFu, more, k * A + i);
+                    bits = ((q < B ? lo : past) | (q + 1 < B ? hi : past) << 8) >> (at & 7);
+                }
 #pragma unroll
                 for (int j = 0; j < VE; ++j) f[(k * A + i) * VE + j] = (bits >> j) & 1u ? f[(k * A + i) * VE + j] : 0.0f;
             }
@@ -208,19 +333,28 @@ template <int DT, int VB, int TPR, int E> __device__ __forceinline__ void drop_r
     for (int k = 0; k < E / 2; ++k) v[k] = __fmul2_rn(v[k], scale);
 }
 
-// v times the parameters of its columns, an access after the other: rows whose parameters have no registers of their own
-template <int DT, int VB, int TPR, int E> __device__ __forceinline__ void times_params(const void* p, bool f32, bool vec, int cols, float2 (&v)[E / 2]) {
-    using R = RowRegs<DT, VB, TPR, E>;
+// v times the parameters of its columns, an access after the other: rows whose parameters have no registers of their own.  With a lead they lie
+// in shared memory as the columns do in the accesses (a block has one lead where it has one group).
+template <int DT, int VB, int TPR, int E> __device__ __forceinline__ void times_params(const void* p, bool f32, bool vec, int cols, const float* shared, float2 (&v)[E / 2]) {
+    using R = Row<DT, VB, TPR, E>;
     float* f = reinterpret_cast<float*>(v);
 #pragma unroll
     for (int i = 0; i < R::NV; ++i) {
         float w[R::VE];
-        if (R::column(i) < cols) {
-            load_params<R::VE>(p, f32, vec, R::column(i), w, 1.0f);
+        if constexpr (VB == kLead) load_params<R::VE>(shared, true, true, R::column(i, 0), w, 1.0f);
+        else if (R::column(i, 0) < cols) load_params<R::VE>(p, f32, vec, R::column(i, 0), w, 1.0f);
+        else continue;
 #pragma unroll
-            for (int j = 0; j < R::VE; ++j) f[i * R::VE + j] *= w[j];
-        }
+        for (int j = 0; j < R::VE; ++j) f[i * R::VE + j] *= w[j];
     }
+}
+template <int TPR, int E> __device__ __forceinline__ void share_params(const void* p, bool f32, int cols, int lead, float* shared) {
+    for (int k = threadIdx.x; k < TPR * E; k += TPR) {
+        float w = 0.0f;
+        if (k >= lead && k - lead < cols) load_params<1>(p, f32, false, k - lead, &w, 1.0f);
+        shared[k] = w;
+    }
+    __syncthreads();
 }
 
 // (sum of v.x, largest v.y) over the TPR threads of a row; buf as for row_sum2
@@ -244,24 +378,27 @@ template <int TPR, int E> constexpr int kBackwardBlocks = std::max(1, (E <= 8 ? 
 
 template <int DT, int VB, int TPR, int E, int FORM>
 __global__ void __launch_bounds__(kForwardThreads<TPR>, kForwardBlocks<TPR, E>) rms_forward_kernel(const RmsArgs a, bool vec8) {
-    using R = RowRegs<DT, VB, TPR, E>;
+    using R = Row<DT, VB, TPR, E>;
     constexpr int P = E / 2, VE = R::VE, kGroups = kForwardThreads<TPR> / TPR;
     // kAhead: the next row is asked for before this one is reduced, where the registers suffice; kFetch: else it is brought to L2
-    constexpr bool kAhead = VB == 16 ? DT == kBF16 || R::NV <= 2 : E == 16 && (TPR == 256 || TPR == 512), kKeep = TPR < 1024 || E < 16, kFetch = !kAhead && TPR >= 128;
+    constexpr bool kAhead = VB != kAny<DT> ? (DT == kBF16 && !(TPR == 1024 && E == 16)) || (DT == kF32 && R::NV <= 2) : E == 16 && (TPR == 256 || TPR == 512), kKeep = TPR < 1024 || E < 16, kFetch = !kAhead && TPR >= 128;
+    extern __shared__ __align__(16) float shared[];       // kLead without kKeep: the weights
     __shared__ float2 buf[2][32];
     __shared__ float tops[FORM == kE4m3 && VE == 1 ? kGroups * TPR * E / 32 : 1];
     const Philox key(a.drop.keys, a.drop.offset, FORM == kDrop ? a.drop.offset_dev : nullptr);
     const int t = threadIdx.x % TPR, g = threadIdx.x / TPR, cols = (int)a.cols, lane = threadIdx.x & 31;
     const float inv_n = 1.0f / (float)a.cols;
     const long long step = (long long)gridDim.x * kGroups;
+    const int lead = VB == kLead ? (int)((reinterpret_cast<uintptr_t>(row_of<DT>(a.x, a.ld_x, (long long)blockIdx.x * kGroups + g)) & 15) / sizeof(typename R::T)) : 0;
     float2 w[P];
-    if constexpr (kKeep) R::params(a.weight, a.weight_f32, a.weight_vec, cols, w, 1.0f);
+    if constexpr (VB == kLead && !kKeep) share_params<TPR, E>(a.weight, a.weight_f32, cols, lead, shared);
+    if constexpr (kKeep) R::params(a.weight, a.weight_f32, a.weight_vec, cols, lead, w);
     typename R::Raw ux[R::NV], us[R::NV];
     const auto ask = [&](long long r) {
         if constexpr (kAhead) {
             const int n = r < a.rows ? cols : 0;
-            R::ask(row_of<DT>(a.x, a.ld_x, r), n, ux);
-            if (a.residual) R::ask(row_of<DT>(a.residual, a.ld_residual, r), n, us);
+            R::ask(Of{a.x, a.ld_x, a.rows}, r, n, lead, ux);
+            if (a.residual) R::ask(Of{a.residual, a.ld_residual, a.rows}, r, n, lead, us);
         }
     };
     ask((long long)blockIdx.x * kGroups + g);
@@ -270,24 +407,29 @@ __global__ void __launch_bounds__(kForwardThreads<TPR>, kForwardBlocks<TPR, E>) 
         const long long r = r0 + g;
         const bool on = r < a.rows;                       // whole groups idle together, but take part in the shuffles and barriers
         float2 h[P];
-        if constexpr (kAhead) R::take(ux, h);
-        else R::load(row_of<DT>(a.x, a.ld_x, r), on ? cols : 0, h);
-        if constexpr (FORM == kDrop) drop_row<DT, VB, TPR, E>(key, a.drop, r, h);
+        if constexpr (kAhead) {
+            R::ends(Of{a.x, a.ld_x, a.rows}, r, on ? cols : 0, lead, ux);
+            R::take(ux, h);
+        } else R::load(Of{a.x, a.ld_x, a.rows}, r, on ? cols : 0, lead, h);
+        if constexpr (FORM == kDrop) drop_row<DT, VB, TPR, E>(key, a.drop, r, lead, h);
         if (a.residual) {
             float2 s[P];
-            if constexpr (kAhead) R::take(us, s);
-            else R::load(row_of<DT>(a.residual, a.ld_residual, r), on ? cols : 0, s);
+            if constexpr (kAhead) {
+                R::ends(Of{a.residual, a.ld_residual, a.rows}, r, on ? cols : 0, lead, us);
+                R::take(us, s);
+            } else R::load(Of{a.residual, a.ld_residual, a.rows}, r, on ? cols : 0, lead, s);
 #pragma unroll
             for (int k = 0; k < P; ++k) h[k] = __fadd2_rn(h[k], s[k]);
         }
+        R::inside(cols, lead, h);
         ask(r + step);
         if constexpr (kFetch) R::fetch(a.x, a.ld_x, a.residual ? a.residual : a.x, a.residual ? a.ld_residual : a.ld_x, r + step, a.rows, cols);
-        if (a.sum && on) R::store(row_of<DT>(a.sum, a.ld_sum, r), cols, h);
+        if (a.sum && on) R::store(row_of<DT>(a.sum, a.ld_sum, r), cols, lead, h);
         float2 sq = make_float2(0.0f, 0.0f);
         float top = 0.0f;
 #pragma unroll
         for (int k = 0; k < P; ++k) sq = __ffma2_rn(h[k], h[k], sq);
-        if constexpr (!kKeep) times_params<DT, VB, TPR, E>(a.weight, a.weight_f32, a.weight_vec, cols, h);
+        if constexpr (!kKeep) times_params<DT, VB, TPR, E>(a.weight, a.weight_f32, a.weight_vec, cols, shared, h);
 #pragma unroll
         for (int k = 0; k < P; ++k) {
             if constexpr (kKeep) h[k] = __fmul2_rn(h[k], w[k]);      // zeros past the last column
@@ -305,7 +447,7 @@ __global__ void __launch_bounds__(kForwardThreads<TPR>, kForwardBlocks<TPR, E>) 
             const float2 rr = make_float2(rstd, rstd);
 #pragma unroll
             for (int k = 0; k < P; ++k) h[k] = __fmul2_rn(h[k], rr);
-            R::store(row_of<DT>(a.y, a.ld_y, r), cols, h);
+            R::store(row_of<DT>(a.y, a.ld_y, r), cols, lead, h);
         } else {
             const float* f = reinterpret_cast<const float*>(h);
             uint8_t* y = static_cast<uint8_t*>(a.y) + r * a.ld_y;
@@ -337,9 +479,10 @@ __global__ void __launch_bounds__(kForwardThreads<TPR>, kForwardBlocks<TPR, E>) 
             float by = __fdividef(1.0f, scale);            // up to 2^126: times rstd it could leave fp32's range
 #pragma unroll
             for (int i = 0; i < R::NV; ++i) {
-                const int c = R::column(i);
+                const int c = R::column(i, lead);
                 if (a.group) {
-                    if constexpr (VE == 1) by = tops[g * (TPR * E / 32) + (c >> shift)];
+                    if constexpr (VB == kLead) {}          // the launch takes these rows an element at a time: groups would not start with accesses
+                    else if constexpr (VE == 1) by = tops[g * (TPR * E / 32) + (c >> shift)];
                     else {
                         float m = 0.0f;
 #pragma unroll
@@ -350,16 +493,17 @@ __global__ void __launch_bounds__(kForwardThreads<TPR>, kForwardBlocks<TPR, E>) 
                         if (on && c < cols && (c & (a.group - 1)) == 0) scales[c >> shift] = scale;
                     }
                 }
-                if (!on || c >= cols) continue;           // behind the shuffles of this access
+                if (!on || !R::any(c, cols)) continue;    // behind the shuffles of this access
                 float q[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) q[j] = j < VE ? f[i * VE + j % VE] * rstd * by : 0.0f;
                 const uint32_t lo = pack_e4m3(q[0], q[1], q[2], q[3]), hi = pack_e4m3(q[4], q[5], q[6], q[7]);
-                if (VE == 8 && vec8) *reinterpret_cast<uint2*>(y + c) = make_uint2(lo, hi);
-                else if (VE == 4 && vec8) *reinterpret_cast<uint32_t*>(y + c) = lo;
+                const bool whole = VB == kLead ? c >= 0 && c + VE <= cols && (reinterpret_cast<uintptr_t>(y + c) & (VE - 1)) == 0 : vec8;
+                if (VE == 8 && whole) *reinterpret_cast<uint2*>(y + c) = make_uint2(lo, hi);
+                else if (VE == 4 && whole) *reinterpret_cast<uint32_t*>(y + c) = lo;
                 else {
 #pragma unroll
-                    for (int j = 0; j < VE; ++j) y[c + j] = (uint8_t)((j < 4 ? lo : hi) >> (8 * (j & 3)));
+                    for (int j = 0; j < VE; ++j) if (VB != kLead || (c + j >= 0 && c + j < cols)) y[c + j] = (uint8_t)((j < 4 ? lo : hi) >> (8 * (j & 3)));
                 }
             }
         }
@@ -368,17 +512,19 @@ __global__ void __launch_bounds__(kForwardThreads<TPR>, kForwardBlocks<TPR, E>) 
 
 template <int DT, int VB, int TPR, int E, int FORM>
 __global__ void __launch_bounds__(kBackwardThreads<TPR, E>, kBackwardBlocks<TPR, E>) rms_backward_kernel(const RmsBackArgs a) {
-    using R = RowRegs<DT, VB, TPR, E>;
+    using R = Row<DT, VB, TPR, E>;
     constexpr int P = E / 2, kThreads = kBackwardThreads<TPR, E>, kGroups = kThreads / TPR;
-    constexpr bool kAhead = VB == 16 && DT == kBF16 && TPR < 1024, kKeep = TPR < 1024 || E == 8, kFetch = !kAhead && (TPR == 1024 || (VB == 16 && TPR >= 128));
+    constexpr bool kAhead = VB != kAny<DT> && DT == kBF16 && TPR < 1024, kKeep = TPR < 1024 || E == 8, kFetch = !kAhead && (TPR == 1024 || (VB != kAny<DT> && TPR >= 128));
     __shared__ float buf[2][32];
-    extern __shared__ float fold[];                       // kGroups > 1: [cols]
+    extern __shared__ __align__(16) float fold[];         // kGroups > 1: [cols]; kLead without kKeep: the weights
     const Philox key(a.drop.keys, a.drop.offset, FORM == kDrop ? a.drop.offset_dev : nullptr);
     const int g = threadIdx.x / TPR, cols = (int)a.cols;
     const float inv_n = 1.0f / (float)a.cols;
     const long long step = (long long)gridDim.x * kGroups;
+    const int lead = VB == kLead ? (int)((reinterpret_cast<uintptr_t>(row_of<DT>(a.h, a.ld_h, (long long)blockIdx.x * kGroups + g)) & 15) / sizeof(typename R::T)) : 0;
     float2 w[P], dw[P];
-    if constexpr (kKeep) R::params(a.weight, a.weight_f32, a.weight_vec, cols, w, 1.0f);
+    if constexpr (VB == kLead && !kKeep) share_params<TPR, E>(a.weight, a.weight_f32, cols, lead, fold);
+    if constexpr (kKeep) R::params(a.weight, a.weight_f32, a.weight_vec, cols, lead, w);
 #pragma unroll
     for (int k = 0; k < P; ++k) dw[k] = make_float2(0.0f, 0.0f);
     int turn = 0;
@@ -387,9 +533,9 @@ __global__ void __launch_bounds__(kBackwardThreads<TPR, E>, kBackwardBlocks<TPR,
     const auto ask = [&](long long r) {
         if constexpr (kAhead) {
             const bool on = r < a.rows;
-            R::ask(row_of<DT>(a.dy, a.ld_dy, r), on ? cols : 0, ud);
-            R::ask(row_of<DT>(a.h, a.ld_h, r), on ? cols : 0, ux);
-            R::ask(row_of<DT>(a.dsum, a.ld_dsum, r), on && a.dsum ? cols : 0, ue);
+            R::ask(Of{a.dy, a.ld_dy, a.rows}, r, on ? cols : 0, lead, ud);
+            R::ask(Of{a.h, a.ld_h, a.rows}, r, on ? cols : 0, lead, ux);
+            R::ask(Of{a.dsum, a.ld_dsum, a.rows}, r, on && a.dsum ? cols : 0, lead, ue);
             next_rstd = on ? a.rstd[r] : 0.0f;
         }
     };
@@ -401,21 +547,28 @@ __global__ void __launch_bounds__(kBackwardThreads<TPR, E>, kBackwardBlocks<TPR,
         float2 d[P], x[P], e[kLate ? 1 : P];
         float rstd;
         if constexpr (kAhead) {
+            R::ends(Of{a.dy, a.ld_dy, a.rows}, r, on ? cols : 0, lead, ud);
             R::take(ud, d);
+            R::ends(Of{a.h, a.ld_h, a.rows}, r, on ? cols : 0, lead, ux);
             R::take(ux, x);
-            if constexpr (!kLate) R::take(ue, e);         // zeros without a dsum
+            if constexpr (!kLate) {
+                R::ends(Of{a.dsum, a.ld_dsum, a.rows}, r, on && a.dsum ? cols : 0, lead, ue);
+                R::take(ue, e);                           // zeros without a dsum
+            }
             rstd = next_rstd;
         } else {
-            R::load(row_of<DT>(a.dy, a.ld_dy, r), on ? cols : 0, d);
-            R::load(row_of<DT>(a.h, a.ld_h, r), on ? cols : 0, x);
+            R::load(Of{a.dy, a.ld_dy, a.rows}, r, on ? cols : 0, lead, d);
+            R::load(Of{a.h, a.ld_h, a.rows}, r, on ? cols : 0, lead, x);
             rstd = on ? a.rstd[r] : 0.0f;
-            if constexpr (!kLate) R::load(row_of<DT>(a.dsum, a.ld_dsum, r), on && a.dsum ? cols : 0, e);
+            if constexpr (!kLate) R::load(Of{a.dsum, a.ld_dsum, a.rows}, r, on && a.dsum ? cols : 0, lead, e);
         }
         if constexpr (kFetch) {
             R::fetch(a.dy, a.ld_dy, a.h, a.ld_h, r + step, a.rows, cols);
-            if constexpr (VB == 16) if (a.dsum) R::fetch(a.dsum, a.ld_dsum, a.dsum, a.ld_dsum, r + step, a.rows, cols);
+            if constexpr (VB != kAny<DT>) if (a.dsum) R::fetch(a.dsum, a.ld_dsum, a.dsum, a.ld_dsum, r + step, a.rows, cols);
         }
         ask(r + step);
+        R::inside(cols, lead, d);
+        R::inside(cols, lead, x);
         const float2 rs = make_float2(rstd, rstd);
         float2 s2 = make_float2(0.0f, 0.0f);
 #pragma unroll
@@ -424,7 +577,7 @@ __global__ void __launch_bounds__(kBackwardThreads<TPR, E>, kBackwardBlocks<TPR,
             dw[k] = __ffma2_rn(d[k], x[k], dw[k]);
             if constexpr (kKeep) d[k] = __fmul2_rn(d[k], w[k]);
         }
-        if constexpr (!kKeep) times_params<DT, VB, TPR, E>(a.weight, a.weight_f32, a.weight_vec, cols, d);
+        if constexpr (!kKeep) times_params<DT, VB, TPR, E>(a.weight, a.weight_f32, a.weight_vec, cols, fold, d);
 #pragma unroll
         for (int k = 0; k < P; ++k) s2 = __ffma2_rn(d[k], x[k], s2);
         const float m2 = -row_sum<TPR, kGroups>(s2.x + s2.y, buf[turn]) * inv_n;
@@ -440,17 +593,17 @@ __global__ void __launch_bounds__(kBackwardThreads<TPR, E>, kBackwardBlocks<TPR,
                 float* f = reinterpret_cast<float*>(d);
 #pragma unroll
                 for (int i = 0; i < R::NV; ++i)
-                    if (on && R::column(i) < cols) {
+                    if (on && R::any(R::column(i, lead), cols)) {
                         float v[R::VE];
-                        R::A::load(reinterpret_cast<const char*>(row_of<DT>(a.dsum, a.ld_dsum, r) + R::column(i)), v);
+                        R::some(Of{a.dsum, a.ld_dsum, a.rows}, r, R::column(i, lead), cols, v);
 #pragma unroll
                         for (int j = 0; j < R::VE; ++j) f[i * R::VE + j] += v[j];
                     }
             }
         }
-        if (on && a.dh) R::store(row_of<DT>(a.dh, a.ld_dh, r), cols, d);
-        if constexpr (FORM == kDrop) drop_row<DT, VB, TPR, E>(key, a.drop, r, d);
-        if (on && a.dx) R::store(row_of<DT>(a.dx, a.ld_dx, r), cols, d);
+        if (on && a.dh) R::store(row_of<DT>(a.dh, a.ld_dh, r), cols, lead, d);
+        if constexpr (FORM == kDrop) drop_row<DT, VB, TPR, E>(key, a.drop, r, lead, d);
+        if (on && a.dx) R::store(row_of<DT>(a.dx, a.ld_dx, r), cols, lead, d);
     }
     if (!a.partials) return;
     float* out = a.partials + (long long)blockIdx.x * a.cols;
@@ -463,8 +616,8 @@ __global__ void __launch_bounds__(kBackwardThreads<TPR, E>, kBackwardBlocks<TPR,
         float* to = k + 1 == kGroups ? out : fold;
 #pragma unroll
         for (int q = 0; q < E; ++q) {
-            const int c = R::column(q / R::VE) + q % R::VE;
-            if (c < cols) to[c] = fw[q] + (k ? fold[c] : 0.0f);
+            const int c = R::column(q / R::VE, lead) + q % R::VE;
+            if (c >= 0 && c < cols) to[c] = fw[q] + (k ? fold[c] : 0.0f);
         }
     }
 }
@@ -615,40 +768,73 @@ bool aligned(const void* p, long long ld, int elem) { return !p || ((uintptr_t)p
 
 constexpr long long kRegisterWidth = 16384;
 
+// Blocks of `rows` rows each, at most `cap`; with a lead, blocks that come round again come to rows of the same lead: those are `period` apart
+unsigned blocks_of(long long rows, int groups, long long cap, int period) {
+    const long long want = (rows + groups - 1) / groups;
+    return (unsigned)(want <= cap ? want : std::max<long long>(cap / period, 1) * period);
+}
+int period_of(long long ld, int elem) {            // rows after which the lead comes again
+    int n = 1;
+    while (ld * elem * n % 16) n *= 2;
+    return n;
+}
+
 template <int DT, int VB, int TPR, int E, int FORM> cudaError_t forward(const RmsArgs& a, int sms, cudaStream_t stream) {
     constexpr int kThreads = kForwardThreads<TPR>, kGroups = kThreads / TPR;
-    const long long want = (a.rows + kGroups - 1) / kGroups, cap = (long long)kForwardBlocks<TPR, E> * sms;
-    const int bytes = VB / RowType<DT>::kBytes;           // that a thread stores of y8 at a time
-    rms_forward_kernel<DT, VB, TPR, E, FORM><<<(unsigned)std::min(want, cap), kThreads, 0, stream>>>(a, (uintptr_t)a.y % bytes == 0 && a.ld_y % bytes == 0);
+    const unsigned grid = blocks_of(a.rows, kGroups, (long long)kForwardBlocks<TPR, E> * sms, VB == kLead ? period_of(a.ld_x, RowType<DT>::kBytes) : 1);
+    const int bytes = VB == kLead ? 1 : VB / RowType<DT>::kBytes;      // that a thread stores of y8 at a time
+    auto kernel = rms_forward_kernel<DT, VB, TPR, E, FORM>;
+    const size_t smem = VB == kLead && TPR == 1024 && E == 16 ? sizeof(float) * TPR * E : 0;      // the weights
+    if (smem) {
+        static PerDeviceOnce once;
+        const cudaError_t e = once.run([&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem); });
+        if (e != cudaSuccess) return e;
+    }
+    kernel<<<grid, kThreads, smem, stream>>>(a, (uintptr_t)a.y % bytes == 0 && a.ld_y % bytes == 0);
     return cudaGetLastError();
 }
 template <int DT, int VB, int TPR, int E, int FORM> cudaError_t backward(const RmsBackArgs& a, int sms, int* used, cudaStream_t stream) {
     constexpr int kThreads = kBackwardThreads<TPR, E>, kGroups = kThreads / TPR;
-    const long long want = (a.rows + kGroups - 1) / kGroups, cap = std::min<long long>((long long)kBackwardBlocks<TPR, E> * sms, rms_partial_rows(a.rows, a.cols));
-    *used = (int)std::min(want, cap);
-    const size_t smem = kGroups > 1 && a.partials ? sizeof(float) * (size_t)a.cols : 0;          // at most 8 KB: these rows have 2048 columns or fewer
-    rms_backward_kernel<DT, VB, TPR, E, FORM><<<(unsigned)*used, kThreads, smem, stream>>>(a);
+    const long long cap = std::min<long long>((long long)kBackwardBlocks<TPR, E> * sms, rms_partial_rows(a.rows, a.cols));
+    *used = (int)blocks_of(a.rows, kGroups, cap, VB == kLead ? period_of(a.ld_h, RowType<DT>::kBytes) : 1);
+    auto kernel = rms_backward_kernel<DT, VB, TPR, E, FORM>;
+    size_t smem = kGroups > 1 && a.partials ? sizeof(float) * (size_t)a.cols : 0;                // at most 8 KB: these rows have 2048 columns or fewer
+    if (VB == kLead && TPR == 1024 && E == 16) {
+        smem = sizeof(float) * TPR * E;                   // the weights
+        static PerDeviceOnce once;
+        const cudaError_t e = once.run([&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem); });
+        if (e != cudaSuccess) return e;
+    }
+    kernel<<<(unsigned)*used, kThreads, smem, stream>>>(a);
     return cudaGetLastError();
 }
 
-// The form for a row of `cols` elements: threads that share it, elements of each
+// The form for a row of `cols` elements, and with a lead up to a vector less one in front of them: threads that share it, elements of each.
+// Of the forms with a lead those stand here that the launches below take.
 template <int DT, int VB, int FORM> cudaError_t forward_by_width(const RmsArgs& a, int sms, cudaStream_t stream) {
-    if (a.cols <= 256) return forward<DT, VB, 32, 8, FORM>(a, sms, stream);
-    if (a.cols <= 512) return forward<DT, VB, 32, 16, FORM>(a, sms, stream);
-    if (a.cols <= 1024) return forward<DT, VB, VB == 16 ? 128 : 64, VB == 16 ? 8 : 16, FORM>(a, sms, stream);
-    if (a.cols <= 2048) return forward<DT, VB, 128, 16, FORM>(a, sms, stream);
-    if (a.cols <= 4096) return forward<DT, VB, 256, 16, FORM>(a, sms, stream);
-    constexpr bool kWords = VB == 16 && DT == kF32;
-    if (a.cols <= 8192) return forward<DT, VB, kWords ? 1024 : 512, kWords ? 8 : 16, FORM>(a, sms, stream);
-    return forward<DT, VB, 1024, 16, FORM>(a, sms, stream);
+    if constexpr (VB == kLead && DT == kF32) return forward<DT, VB, 256, 16, FORM>(a, sms, stream);
+    else {
+        constexpr bool kVector = VB != kAny<DT>, kWords = kVector && DT == kF32;
+        const long long width = a.cols + (VB == kLead ? RowType<DT>::kVec - 1 : 0);
+        if (width <= 256) return forward<DT, VB, 32, 8, FORM>(a, sms, stream);
+        if (width <= 512) return forward<DT, VB, 32, 16, FORM>(a, sms, stream);
+        if (width <= 1024) return forward<DT, VB, kVector ? 128 : 64, kVector ? 8 : 16, FORM>(a, sms, stream);
+        if (width <= 2048) return forward<DT, VB, 128, 16, FORM>(a, sms, stream);
+        if (width <= 4096) return forward<DT, VB, 256, 16, FORM>(a, sms, stream);
+        if (width <= 8192) return forward<DT, VB, kWords ? 1024 : 512, kWords ? 8 : 16, FORM>(a, sms, stream);
+        return forward<DT, VB, 1024, 16, FORM>(a, sms, stream);
+    }
 }
 template <int DT, int VB, int FORM> cudaError_t backward_by_width(const RmsBackArgs& a, int sms, int* used, cudaStream_t stream) {
-    if (a.cols <= 256) return backward<DT, VB, 32, 8, FORM>(a, sms, used, stream);
-    if (a.cols <= 512) return backward<DT, VB, 64, 8, FORM>(a, sms, used, stream);
-    if (a.cols <= 1024) return backward<DT, VB, 128, 8, FORM>(a, sms, used, stream);
-    if (a.cols <= 2048) return backward<DT, VB, 256, 8, FORM>(a, sms, used, stream);
-    if (a.cols <= 4096) return backward<DT, VB, 256, 16, FORM>(a, sms, used, stream);
-    if (a.cols <= 8192) return backward<DT, VB, VB == 16 ? 512 : 1024, VB == 16 ? 16 : 8, FORM>(a, sms, used, stream);
+    const long long width = a.cols + (VB == kLead ? RowType<DT>::kVec - 1 : 0);
+    if (width <= 256) return backward<DT, VB, 32, 8, FORM>(a, sms, used, stream);
+    if (width <= 512) return backward<DT, VB, 64, 8, FORM>(a, sms, used, stream);
+    if (width <= 1024) return backward<DT, VB, 128, 8, FORM>(a, sms, used, stream);
+    if (width <= 2048) return backward<DT, VB, 256, 8, FORM>(a, sms, used, stream);
+    // bf16 an element at a time, rows of two leads: 8000 x 3001 by (256, 16) 259 us, (512, 8) 142; fp32 61 and 90
+    constexpr bool kHalves = VB == kAny<DT> && DT == kBF16;
+    if (width <= 4096) return backward<DT, VB, kHalves ? 512 : 256, kHalves ? 8 : 16, FORM>(a, sms, used, stream);
+    if constexpr (VB != kLead) { if (width <= 8192) return backward<DT, VB, VB == 16 ? 512 : 1024, VB == 16 ? 16 : 8, FORM>(a, sms, used, stream); }
     return backward<DT, VB, 1024, 16, FORM>(a, sms, used, stream);
 }
 template <int DT, int VB> cudaError_t forward_by_form(const RmsArgs& a, int sms, cudaStream_t stream) {
@@ -658,6 +844,26 @@ template <int DT, int VB> cudaError_t forward_by_form(const RmsArgs& a, int sms,
 template <int DT, int VB> cudaError_t backward_by_form(const RmsBackArgs& a, int sms, int* used, cudaStream_t stream) {
     return a.drop.limit && a.dx ? backward_by_width<DT, VB, kDrop>(a, sms, used, stream) : backward_by_width<DT, VB, kPlain>(a, sms, used, stream);
 }
+template <int DT> cudaError_t forward_by_access(const RmsArgs& a, int access, int sms, cudaStream_t stream) {
+    return access == 16 ? forward_by_form<DT, 16>(a, sms, stream) : access == kLead ? forward_by_form<DT, kLead>(a, sms, stream) : forward_by_form<DT, kAny<DT>>(a, sms, stream);
+}
+template <int DT> cudaError_t backward_by_access(const RmsBackArgs& a, int access, int sms, int* used, cudaStream_t stream) {
+    if constexpr (DT == kBF16) { if (access == kLead) return backward_by_form<DT, kLead>(a, sms, used, stream); }
+    return access == 16 ? backward_by_form<DT, 16>(a, sms, used, stream) : backward_by_form<DT, kAny<DT>>(a, sms, used, stream);
+}
+
+// How the rows of some matrices can be accessed, all alike: 16, kLead or (for more than one element's bytes) kAny
+struct Matrices {
+    int elem, start = -1, step = -1;
+    bool same = true;
+    void add(const void* p, long long ld) {
+        if (!p) return;
+        const int at = (int)((uintptr_t)p % 16), by = (int)(ld * elem % 16);
+        if (start < 0) { start = at; step = by; }
+        same = same && at == start && by == step;
+    }
+    int access(long long cols) const { return !same || cols * elem < 16 ? elem : start == 0 && step == 0 && cols * elem % 16 == 0 ? 16 : kLead; }
+};
 
 template <int DT> cudaError_t dropout(const DropoutArgs& a, bool vec, int sms, cudaStream_t stream) {
     const long long blocks = (a.cols + 7) / 8;
@@ -689,9 +895,19 @@ cudaError_t launch_rms_forward(RmsArgs a, int dtype, int sms, cudaStream_t strea
     const bool e8 = a.scales != nullptr;
     const bool vec = aligned(a.x, a.ld_x, e) && aligned(a.residual, a.ld_residual, e) && aligned(a.sum, a.ld_sum, e) && (e8 || aligned(a.y, a.ld_y, e));
     if (a.cols <= kRegisterWidth) {
-        const bool all = vec && a.cols * e % 16 == 0;
-        if (dtype == kF32) return all ? forward_by_form<kF32, 16>(a, sms, stream) : forward_by_form<kF32, 4>(a, sms, stream);
-        return all ? forward_by_form<kBF16, 16>(a, sms, stream) : forward_by_form<kBF16, 2>(a, sms, stream);
+        Matrices m = {e};
+        m.add(a.x, a.ld_x);
+        m.add(a.residual, a.ld_residual);
+        m.add(a.sum, a.ld_sum);
+        if (!e8) m.add(a.y, a.ld_y);
+        // With a lead, groups of columns would start inside accesses, and the widest rows have no room for it.  Else, us an element at a time and with
+        // it: bf16 16000 x 999 35.5 and 19.7, 8000 x 3001 49.1 and 43.1, 3000 x 9001 122 and 93; but 2047 x 8191, where it takes the next form,
+        // 21.4 and 35.9.  fp32, whose single elements fill a line a warp, 8000 x 3001 44.2 and 35.4, but 4097 x 1001 5.9 and 6.8, 4000 x 5001 with
+        // dropout 54.7 and 75.7.
+        int access = m.access(a.cols);
+        const long long width = a.cols + 16 / e - 1;
+        if (access == kLead && ((e8 && a.group) || width > kRegisterWidth || (dtype == kF32 ? a.cols <= 2048 || width > 4096 : a.cols <= 8192 && width > 8192))) access = e;
+        return dtype == kF32 ? forward_by_access<kF32>(a, access, sms, stream) : forward_by_access<kBF16>(a, access, sms, stream);
     }
     const bool vec8 = (uintptr_t)a.y % 8 == 0 && a.ld_y % 8 == 0;
     const unsigned grid = (unsigned)std::min<long long>(a.rows, 4ll * sms);
@@ -713,9 +929,18 @@ cudaError_t launch_rms_backward(RmsBackArgs a, int dtype, void* dweight, int sms
     cudaError_t err = cudaSuccess;
     const bool vec = aligned(a.dy, a.ld_dy, e) && aligned(a.h, a.ld_h, e) && aligned(a.dsum, a.ld_dsum, e) && aligned(a.dh, a.ld_dh, e) && aligned(a.dx, a.ld_dx, e);
     if (a.rows > 0 && a.cols <= kRegisterWidth) {
-        const bool all = vec && a.cols * e % 16 == 0;
-        if (dtype == kF32) err = all ? backward_by_form<kF32, 16>(a, sms, &used, stream) : backward_by_form<kF32, 4>(a, sms, &used, stream);
-        else err = all ? backward_by_form<kBF16, 16>(a, sms, &used, stream) : backward_by_form<kBF16, 2>(a, sms, &used, stream);
+        Matrices m = {e};
+        m.add(a.dy, a.ld_dy);
+        m.add(a.h, a.ld_h);
+        m.add(a.dsum, a.ld_dsum);
+        m.add(a.dh, a.ld_dh);
+        m.add(a.dx, a.ld_dx);
+        // As above: bf16 16000 x 999 45.7 and 33.5, 16000 x 1801 87.8 and 56.0, 3000 x 9001 131 and 89, but 200 x 5001 8.8 and 12.2, 8000 x 5001
+        // with dropout 167 and 191; fp32 8000 x 3001 76.2 and 77.5, 4097 x 1001 18.4 and 23.6
+        int access = m.access(a.cols);
+        const long long width = a.cols + 16 / e - 1;
+        if (access == kLead && (dtype == kF32 || width > kRegisterWidth || (width > 4096 && a.cols <= 8192))) access = e;
+        err = dtype == kF32 ? backward_by_access<kF32>(a, access, sms, &used, stream) : backward_by_access<kBF16>(a, access, sms, &used, stream);
     } else if (a.rows > 0) {
         if (a.partials) {
             used = rms_partial_rows(a.rows, a.cols);
