@@ -206,3 +206,33 @@ def test_gradient_against_differences():
             a, b = list(args), list(args)
             a[k], b[k] = up.reshape(args[k].shape), down.reshape(args[k].shape)
             assert abs((loss(*a) - loss(*b)) / (2 * step) - flat[i]) < 1e-4
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("cols", [9, 17, 255, 505, 1001, 2041, 3001, 5001, 9001, 16377, 16383])
+def test_rows_do_not_see_their_neighbours(cols, dtype):
+    """Every other row is NaN and Inf; the rows between, and what lies before and behind the matrix, stay as they are."""
+    import torch
+    import paper_2102_08124_b200 as tm
+    kind, rows = getattr(torch, dtype), 37
+    g = torch.Generator("cuda").manual_seed(cols)
+    flat = lambda: torch.randn(rows * cols + 32, device="cuda", generator=g).to(kind)
+    for shift in (0, 3):
+        stores = {k: flat() for k in ("x", "r", "dy", "e")}
+        part = {k: t[16 + shift:16 + shift + rows * cols].view(rows, cols) for k, t in stores.items()}
+        for k, t in part.items():
+            t[1::2] = float("nan")
+            t[1::2, ::2] = float("inf")
+        w = torch.rand(cols, device="cuda", generator=g)
+        out = {k: torch.full((rows * cols + 32,), 7.0, device="cuda", dtype=kind) for k in ("y", "s", "dh", "dx")}
+        o = {k: t[16 + shift:16 + shift + rows * cols].view(rows, cols) for k, t in out.items()}
+        _, _, rstd = tm.tm_rms_norm(part["x"], w, residual=part["r"], p=0.3, seed=1, y=o["y"], sum_out=o["s"])
+        tm.tm_rms_norm_backward(part["dy"], o["s"], rstd, w, dsum=part["e"], p=0.3, seed=1, dh=o["dh"], dx=o["dx"])
+        alone = {k: t.clone().nan_to_num(0.0, 0.0, 0.0) for k, t in part.items()}
+        y, s, r2 = tm.tm_rms_norm(alone["x"], w, residual=alone["r"], p=0.3, seed=1)
+        dh, dx, _ = tm.tm_rms_norm_backward(alone["dy"], s, r2, w, dsum=alone["e"], p=0.3, seed=1)
+        for got, want in ((o["y"], y), (o["s"], s), (o["dh"], dh), (o["dx"], dx)):
+            # the same kernel or one that adds a row's terms in another order, of which the row's factor holds 2^-18
+            assert torch.allclose(got[::2].float(), want[::2].float(), rtol=2.0 ** -7 if dtype == "bfloat16" else 2.0 ** -16, atol=1e-5)
+        for t in out.values():
+            assert bool((t[:16 + shift] == 7).all()) and bool((t[16 + shift + rows * cols:] == 7).all())
