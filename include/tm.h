@@ -337,7 +337,7 @@ int tm_distill_loss_grad(const void* logits, int dtype, int64_t rows, int64_t vo
  * tm_rms_norm -- h = d(x) + residual (p = 0: d(x) = x; residual NULL: none); over the columns of every row
  * rstd = 1 / sqrt(mean(h^2) + eps), y = h * rstd * weight (cols entries of weight_dtype, NULL for ones).  sum_out (may be NULL) receives h
  * rounded to dtype, rstd_out (rows floats, may be NULL) rstd; y comes from h before rounding.  y or sum_out may lie on x or residual.
- * With cols 0 nothing is written.
+ * The squares are summed in fp32 (magnitudes up to 2^63 / sqrt(cols)).  With cols 0 nothing is written.
  *
  * tm_rms_norm_e4m3 -- the same without dropout, y in 8 bits (e4m3: four bits of exponent, three of mantissa, largest value 448) with a scale for
  * every `group` columns of a row (32, 64 or 128; the last may have fewer; 0: one for the row): scale = max(max |y| / 448, 2^-126),

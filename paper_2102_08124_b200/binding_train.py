@@ -19,10 +19,11 @@ TM_TOP_MAX = 256
 _ready = None
 _torch = None              # torch, once a call needed it: importing this package alone does not import torch
 _raw_stream = None
+_current_device = None
 
 
 def _lib():
-    global _ready, _torch, _raw_stream
+    global _ready, _torch, _raw_stream, _current_device
     if _ready is None:
         import torch
         lib = binding.load_library()
@@ -40,6 +41,7 @@ def _lib():
         _torch = torch
         # the address of the current stream without a Stream object around it (2 us less a call), where this torch has it
         _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+        _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
         _ready = lib
     return _ready
 
@@ -48,7 +50,7 @@ def _call(fn, device, *args):
     """fn(*args, torch's current stream) with `device` current."""
     index = device.index
     s = _raw_stream(index)
-    if _torch.cuda.current_device() == index:
+    if _current_device() == index:
         rc = fn(*args, s)
     else:
         with _torch.cuda.device(device):

@@ -185,6 +185,7 @@ struct RmsBackArgs {
     DropSpec drop;
     void *dh, *dx;                              // one of them or both
     float* partials;                            // rms_partial_rows() rows of cols floats, or null
+    void* dweight;                              // or null (set by the launch: the blocks are one cluster that adds up its sums itself)
 };
 int rms_partial_rows(long long rows, long long cols);
 cudaError_t launch_dropout(const DropoutArgs& a, int dtype, int sms, cudaStream_t stream);
