@@ -185,11 +185,18 @@ constexpr int kPlain = 0, kDrop = 1, kE4m3 = 2;      // forms of the kernels bel
 constexpr int kLead = 0;
 template <int DT> constexpr int kAny = RowType<DT>::kBytes;
 
+// A row's address from 32-bit numbers is one instruction; matrices of more rows or longer pitches go to the wide kernels
+template <int DT> __device__ __forceinline__ const typename RowType<DT>::T* row_at(const void* p, uint32_t pitch, uint32_t r) {
+    return reinterpret_cast<const typename RowType<DT>::T*>(static_cast<const char*>(p) + (unsigned long long)pitch * r);
+}
+template <int DT> __device__ __forceinline__ typename RowType<DT>::T* row_at(void* p, uint32_t pitch, uint32_t r) {
+    return reinterpret_cast<typename RowType<DT>::T*>(static_cast<char*>(p) + (unsigned long long)pitch * r);
+}
 // A matrix that is read
 struct Of {
     const void* p;
-    long long ld, rows;
-    template <int DT> __device__ __forceinline__ const typename RowType<DT>::T* row(long long r) const { return row_of<DT>(p, ld, r); }
+    uint32_t pitch, rows;
+    template <int DT> __device__ __forceinline__ const typename RowType<DT>::T* row(uint32_t r) const { return row_at<DT>(p, pitch, r); }
 };
 
 // A vector from column c on, an element at a time: at the matrix's very first and last elements
@@ -209,14 +216,14 @@ template <int DT, int VB, int TPR, int E> struct Row : RowRegs<DT, VB, TPR, E> {
     using T = typename RowType<DT>::T;
     using Raw = typename R::Raw;
     static __device__ __forceinline__ int column(int i, int) { return R::column(i); }
-    static __device__ __forceinline__ void load(const Of& m, long long r, int cols, int, float2 (&v)[E / 2]) { R::load(m.row<DT>(r), cols, v); }
-    static __device__ __forceinline__ void ask(const Of& m, long long r, int cols, int, Raw (&u)[R::NV]) { R::ask(m.row<DT>(r), cols, u); }
+    static __device__ __forceinline__ void load(const Of& m, uint32_t r, int cols, int, float2 (&v)[E / 2]) { R::load(m.row<DT>(r), cols, v); }
+    static __device__ __forceinline__ void ask(const Of& m, uint32_t r, int cols, int, Raw (&u)[R::NV]) { R::ask(m.row<DT>(r), cols, u); }
     static __device__ __forceinline__ void ends(const Of&, long long, int, int, Raw (&)[R::NV]) {}
     static __device__ __forceinline__ void inside(int, int, float2 (&)[E / 2]) {}
     static __device__ __forceinline__ void store(T* row, int cols, int, const float2 (&v)[E / 2]) { R::store(row, cols, v); }
     static __device__ __forceinline__ void params(const void* p, bool f32, bool vec, int cols, int, float2 (&v)[E / 2]) { R::params(p, f32, vec, cols, v, 1.0f); }
     // VE values of row from column c on
-    static __device__ __forceinline__ void some(const Of& m, long long r, int c, int, float* v) { R::A::load(reinterpret_cast<const char*>(m.row<DT>(r) + c), v); }
+    static __device__ __forceinline__ void some(const Of& m, uint32_t r, int c, int, float* v) { R::A::load(reinterpret_cast<const char*>(m.row<DT>(r) + c), v); }
     static __device__ __forceinline__ bool any(int c, int cols) { return c < cols; }
 };
 template <int DT, int TPR, int E> struct Row<DT, kLead, TPR, E> : RowRegs<DT, 16, TPR, E> {
@@ -228,15 +235,15 @@ template <int DT, int TPR, int E> struct Row<DT, kLead, TPR, E> : RowRegs<DT, 16
     static __device__ __forceinline__ bool any(int c, int cols) { return cols > 0 && c + VE > 0 && c < cols; }      // cols is 0 where there is no row
     // Vectors at a row's ends reach into its neighbours (rows are a vector long at least), and are read whole; but for those that would lie before the
     // matrix's first element or behind its last one, whose elements ends() adds
-    static __device__ __forceinline__ bool whole(long long r, long long rows, int c, int cols) {
+    static __device__ __forceinline__ bool whole(uint32_t r, uint32_t rows, int c, int cols) {
         return any(c, cols) && (c >= 0 || r > 0) && (c + VE <= cols || r + 1 < rows);
     }
-    static __device__ __forceinline__ uint4 vector(const Of& m, long long r, int c, int cols) {
+    static __device__ __forceinline__ uint4 vector(const Of& m, uint32_t r, int c, int cols) {
         uint4 u = make_uint4(0, 0, 0, 0);
         if (whole(r, m.rows, c, cols)) u = *reinterpret_cast<const uint4*>(m.row<DT>(r) + c);
         return u;
     }
-    static __device__ __forceinline__ void ends(const Of& m, long long r, int cols, int lead, uint4 (&u)[NV]) {
+    static __device__ __forceinline__ void ends(const Of& m, uint32_t r, int cols, int lead, uint4 (&u)[NV]) {
         if (r > 0 && r + 1 < m.rows) return;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
@@ -244,17 +251,17 @@ template <int DT, int TPR, int E> struct Row<DT, kLead, TPR, E> : RowRegs<DT, 16
             if (any(c, cols) && !whole(r, m.rows, c, cols)) u[i] = first_or_last<DT>(m.row<DT>(r), c, cols);
         }
     }
-    static __device__ __forceinline__ void ask(const Of& m, long long r, int cols, int lead, uint4 (&u)[NV]) {
+    static __device__ __forceinline__ void ask(const Of& m, uint32_t r, int cols, int lead, uint4 (&u)[NV]) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) u[i] = vector(m, r, column(i, lead), cols);
     }
-    static __device__ __forceinline__ void load(const Of& m, long long r, int cols, int lead, float2 (&v)[E / 2]) {
+    static __device__ __forceinline__ void load(const Of& m, uint32_t r, int cols, int lead, float2 (&v)[E / 2]) {
         uint4 u[NV];
         ask(m, r, cols, lead, u);
         ends(m, r, cols, lead, u);
         R::take(u, v);
     }
-    static __device__ __forceinline__ void some(const Of& m, long long r, int c, int cols, float* v) {
+    static __device__ __forceinline__ void some(const Of& m, uint32_t r, int c, int cols, float* v) {
         uint4 u = vector(m, r, c, cols);
         if (any(c, cols) && !whole(r, m.rows, c, cols)) u = first_or_last<DT>(m.row<DT>(r), c, cols);
         unpack_vector<DT>(u, v);
@@ -293,20 +300,26 @@ template <int DT, int TPR, int E> struct Row<DT, kLead, TPR, E> : RowRegs<DT, 16
     }
 };
 
+// brings row r of two matrices to L2, a line a thread: half the threads cover a row of 16 elements a thread
+template <int DT, int TPR> __device__ __forceinline__ void fetch_rows(const void* a, uint32_t pitch_a, const void* b, uint32_t pitch_b, uint32_t r, uint32_t rows, int cols) {
+    const int t = threadIdx.x % TPR, c = (t & (TPR / 2 - 1)) * (128 / RowType<DT>::kBytes);
+    if (r < rows && c < cols) asm volatile("prefetch.global.L2 [%0];" ::"l"((t < TPR / 2 ? row_at<DT>(a, pitch_a, r) : row_at<DT>(b, pitch_b, r)) + c));
+}
+
 // Dropout of what TPR >= 32 threads hold of a row.  A warp's lanes work out one block of eight columns each; accesses that are narrower than a
 // block, or start inside one, take their columns' bits from the lanes that have them (with a lead, an access touches one block more: lane i has
 // access i's).
-template <int DT, int VB, int TPR, int E> __device__ __forceinline__ void drop_row(const Philox& key, const DropSpec& d, long long r, int lead, float2 (&v)[E / 2]) {
+template <int DT, int VB, int TPR, int E> __device__ __forceinline__ void drop_row(const Philox& key, const DropSpec& d, uint32_t r, int lead, float2 (&v)[E / 2]) {
     using R = Row<DT, VB, TPR, E>;
     constexpr int VE = R::VE, NV = R::NV, A = 8 / VE, B = 4 * VE;      // accesses that a warp's 32 blocks are, and blocks of each
     float* f = reinterpret_cast<float*>(v);
     const int t = threadIdx.x % TPR, lane = threadIdx.x & 31;
     const auto first = [&](int i) { return (i * TPR + t - lane) * VE - lead; };      // the warp's first column in access i
     uint32_t more = 0;
-    if constexpr (VB == kLead) more = kept_bits(key((uint32_t)((first(min(lane, NV - 1)) >> 3) + B), (uint32_t)r), d.limit);
+    if constexpr (VB == kLead) more = kept_bits(key((uint32_t)((first(min(lane, NV - 1)) >> 3) + B), r), d.limit);
 #pragma unroll
     for (int k = 0; k < NV / A; ++k) {
-        const uint4 w = key((uint32_t)((first(k * A + lane / B) >> 3) + lane % B), (uint32_t)r);
+        const uint4 w = key((uint32_t)((first(k * A + lane / B) >> 3) + lane % B), r);
         if constexpr (VE == 8 && VB != kLead) {
             const uint32_t high = d.limit << 16, u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
@@ -388,43 +401,45 @@ __global__ void __launch_bounds__(kForwardThreads<TPR>, kForwardBlocks<TPR, E>) 
     const Philox key(a.drop.keys, a.drop.offset, FORM == kDrop ? a.drop.offset_dev : nullptr);
     const int t = threadIdx.x % TPR, g = threadIdx.x / TPR, cols = (int)a.cols, lane = threadIdx.x & 31;
     const float inv_n = 1.0f / (float)a.cols;
-    const long long step = (long long)gridDim.x * kGroups;
-    const int lead = VB == kLead ? (int)((reinterpret_cast<uintptr_t>(row_of<DT>(a.x, a.ld_x, (long long)blockIdx.x * kGroups + g)) & 15) / sizeof(typename R::T)) : 0;
+    const uint32_t rows = (uint32_t)a.rows, step = gridDim.x * kGroups;
+    constexpr uint32_t B = RowType<DT>::kBytes;
+    const uint32_t pitch_x = (uint32_t)a.ld_x * B, pitch_residual = (uint32_t)a.ld_residual * B, pitch_sum = (uint32_t)a.ld_sum * B, pitch_y = (uint32_t)a.ld_y * B;
+    const int lead = VB == kLead ? (int)((reinterpret_cast<uintptr_t>(row_at<DT>(a.x, pitch_x, blockIdx.x * kGroups + g)) & 15) / sizeof(typename R::T)) : 0;
     float2 w[P];
     if constexpr (VB == kLead && !kKeep) share_params<TPR, E>(a.weight, a.weight_f32, cols, lead, shared);
     if constexpr (kKeep) R::params(a.weight, a.weight_f32, a.weight_vec, cols, lead, w);
     typename R::Raw ux[R::NV], us[R::NV];
-    const auto ask = [&](long long r) {
+    const auto ask = [&](uint32_t r) {
         if constexpr (kAhead) {
-            const int n = r < a.rows ? cols : 0;
-            R::ask(Of{a.x, a.ld_x, a.rows}, r, n, lead, ux);
-            if (a.residual) R::ask(Of{a.residual, a.ld_residual, a.rows}, r, n, lead, us);
+            const int n = r < rows ? cols : 0;
+            R::ask(Of{a.x, pitch_x, rows}, r, n, lead, ux);
+            if (a.residual) R::ask(Of{a.residual, pitch_residual, rows}, r, n, lead, us);
         }
     };
-    ask((long long)blockIdx.x * kGroups + g);
+    ask(blockIdx.x * kGroups + g);
     int turn = 0;
-    for (long long r0 = (long long)blockIdx.x * kGroups; r0 < a.rows; r0 += step, turn ^= 1) {
-        const long long r = r0 + g;
-        const bool on = r < a.rows;                       // whole groups idle together, but take part in the shuffles and barriers
+    for (uint32_t r0 = blockIdx.x * kGroups; r0 < rows; r0 += step, turn ^= 1) {
+        const uint32_t r = r0 + g;
+        const bool on = r < rows;                       // whole groups idle together, but take part in the shuffles and barriers
         float2 h[P];
         if constexpr (kAhead) {
-            R::ends(Of{a.x, a.ld_x, a.rows}, r, on ? cols : 0, lead, ux);
+            R::ends(Of{a.x, pitch_x, rows}, r, on ? cols : 0, lead, ux);
             R::take(ux, h);
-        } else R::load(Of{a.x, a.ld_x, a.rows}, r, on ? cols : 0, lead, h);
+        } else R::load(Of{a.x, pitch_x, rows}, r, on ? cols : 0, lead, h);
         if constexpr (FORM == kDrop) drop_row<DT, VB, TPR, E>(key, a.drop, r, lead, h);
         if (a.residual) {
             float2 s[P];
             if constexpr (kAhead) {
-                R::ends(Of{a.residual, a.ld_residual, a.rows}, r, on ? cols : 0, lead, us);
+                R::ends(Of{a.residual, pitch_residual, rows}, r, on ? cols : 0, lead, us);
                 R::take(us, s);
-            } else R::load(Of{a.residual, a.ld_residual, a.rows}, r, on ? cols : 0, lead, s);
+            } else R::load(Of{a.residual, pitch_residual, rows}, r, on ? cols : 0, lead, s);
 #pragma unroll
             for (int k = 0; k < P; ++k) h[k] = __fadd2_rn(h[k], s[k]);
         }
         R::inside(cols, lead, h);
         ask(r + step);
-        if constexpr (kFetch) R::fetch(a.x, a.ld_x, a.residual ? a.residual : a.x, a.residual ? a.ld_residual : a.ld_x, r + step, a.rows, cols);
-        if (a.sum && on) R::store(row_of<DT>(a.sum, a.ld_sum, r), cols, lead, h);
+        if constexpr (kFetch) fetch_rows<DT, TPR>(a.x, pitch_x, a.residual ? a.residual : a.x, a.residual ? pitch_residual : pitch_x, r + step, rows, cols);
+        if (a.sum && on) R::store(row_at<DT>(a.sum, pitch_sum, r), cols, lead, h);
         float2 sq = make_float2(0.0f, 0.0f);
         float top = 0.0f;
 #pragma unroll
@@ -447,12 +462,12 @@ __global__ void __launch_bounds__(kForwardThreads<TPR>, kForwardBlocks<TPR, E>) 
             const float2 rr = make_float2(rstd, rstd);
 #pragma unroll
             for (int k = 0; k < P; ++k) h[k] = __fmul2_rn(h[k], rr);
-            R::store(row_of<DT>(a.y, a.ld_y, r), cols, lead, h);
+            R::store(row_at<DT>(a.y, pitch_y, r), cols, lead, h);
         } else {
             const float* f = reinterpret_cast<const float*>(h);
-            uint8_t* y = static_cast<uint8_t*>(a.y) + r * a.ld_y;
+            uint8_t* y = static_cast<uint8_t*>(a.y) + (unsigned long long)(uint32_t)a.ld_y * r;
             const int shift = __ffs(a.group) - 1;          // a.group is a power of two, or 0
-            float* scales = a.scales + r * (a.group ? (cols + a.group - 1) >> shift : 1);
+            float* scales = a.scales + (unsigned long long)r * (uint32_t)(a.group ? (cols + a.group - 1) >> shift : 1);
             float scale = scale_of(top * rstd);
             if (a.group == 0 && t == 0 && on) scales[0] = scale;
             if (VE == 1 && a.group) {                     // a warp's accesses are 32 columns each
@@ -522,8 +537,10 @@ __global__ void __launch_bounds__(kBackwardThreads<TPR, E>, kBackwardBlocks<TPR,
     const Philox key(a.drop.keys, a.drop.offset, FORM == kDrop ? a.drop.offset_dev : nullptr);
     const int g = threadIdx.x / TPR, cols = (int)a.cols;
     const float inv_n = 1.0f / (float)a.cols;
-    const long long step = (long long)gridDim.x * kGroups;
-    const int lead = VB == kLead ? (int)((reinterpret_cast<uintptr_t>(row_of<DT>(a.h, a.ld_h, (long long)blockIdx.x * kGroups + g)) & 15) / sizeof(typename R::T)) : 0;
+    const uint32_t rows = (uint32_t)a.rows, step = gridDim.x * kGroups;
+    constexpr uint32_t B = RowType<DT>::kBytes;
+    const uint32_t pitch_dy = (uint32_t)a.ld_dy * B, pitch_h = (uint32_t)a.ld_h * B, pitch_dsum = (uint32_t)a.ld_dsum * B, pitch_dh = (uint32_t)a.ld_dh * B, pitch_dx = (uint32_t)a.ld_dx * B;
+    const int lead = VB == kLead ? (int)((reinterpret_cast<uintptr_t>(row_at<DT>(a.h, pitch_h, blockIdx.x * kGroups + g)) & 15) / sizeof(typename R::T)) : 0;
     float2 w[P], dw[P];
     if constexpr (VB == kLead && !kKeep) share_params<TPR, E>(a.weight, a.weight_f32, cols, lead, fold);
     if constexpr (kKeep) R::params(a.weight, a.weight_f32, a.weight_vec, cols, lead, w);
@@ -532,41 +549,41 @@ __global__ void __launch_bounds__(kBackwardThreads<TPR, E>, kBackwardBlocks<TPR,
     int turn = 0;
     typename R::Raw ud[R::NV], ux[R::NV], ue[R::NV];
     float next_rstd = 0.0f;
-    const auto ask = [&](long long r) {
+    const auto ask = [&](uint32_t r) {
         if constexpr (kAhead) {
-            const bool on = r < a.rows;
-            R::ask(Of{a.dy, a.ld_dy, a.rows}, r, on ? cols : 0, lead, ud);
-            R::ask(Of{a.h, a.ld_h, a.rows}, r, on ? cols : 0, lead, ux);
-            R::ask(Of{a.dsum, a.ld_dsum, a.rows}, r, on && a.dsum ? cols : 0, lead, ue);
+            const bool on = r < rows;
+            R::ask(Of{a.dy, pitch_dy, rows}, r, on ? cols : 0, lead, ud);
+            R::ask(Of{a.h, pitch_h, rows}, r, on ? cols : 0, lead, ux);
+            R::ask(Of{a.dsum, pitch_dsum, rows}, r, on && a.dsum ? cols : 0, lead, ue);
             next_rstd = on ? a.rstd[r] : 0.0f;
         }
     };
-    ask((long long)blockIdx.x * kGroups + g);
-    for (long long r0 = (long long)blockIdx.x * kGroups; r0 < a.rows; r0 += step, turn ^= 1) {
-        const long long r = r0 + g;
-        const bool on = r < a.rows;
+    ask(blockIdx.x * kGroups + g);
+    for (uint32_t r0 = blockIdx.x * kGroups; r0 < rows; r0 += step, turn ^= 1) {
+        const uint32_t r = r0 + g;
+        const bool on = r < rows;
         constexpr bool kLate = TPR == 1024;               // dsum is read behind the reduction
         float2 d[P], x[P], e[kLate ? 1 : P];
         float rstd;
         if constexpr (kAhead) {
-            R::ends(Of{a.dy, a.ld_dy, a.rows}, r, on ? cols : 0, lead, ud);
+            R::ends(Of{a.dy, pitch_dy, rows}, r, on ? cols : 0, lead, ud);
             R::take(ud, d);
-            R::ends(Of{a.h, a.ld_h, a.rows}, r, on ? cols : 0, lead, ux);
+            R::ends(Of{a.h, pitch_h, rows}, r, on ? cols : 0, lead, ux);
             R::take(ux, x);
             if constexpr (!kLate) {
-                R::ends(Of{a.dsum, a.ld_dsum, a.rows}, r, on && a.dsum ? cols : 0, lead, ue);
+                R::ends(Of{a.dsum, pitch_dsum, rows}, r, on && a.dsum ? cols : 0, lead, ue);
                 R::take(ue, e);                           // zeros without a dsum
             }
             rstd = next_rstd;
         } else {
-            R::load(Of{a.dy, a.ld_dy, a.rows}, r, on ? cols : 0, lead, d);
-            R::load(Of{a.h, a.ld_h, a.rows}, r, on ? cols : 0, lead, x);
+            R::load(Of{a.dy, pitch_dy, rows}, r, on ? cols : 0, lead, d);
+            R::load(Of{a.h, pitch_h, rows}, r, on ? cols : 0, lead, x);
             rstd = on ? a.rstd[r] : 0.0f;
-            if constexpr (!kLate) R::load(Of{a.dsum, a.ld_dsum, a.rows}, r, on && a.dsum ? cols : 0, lead, e);
+            if constexpr (!kLate) R::load(Of{a.dsum, pitch_dsum, rows}, r, on && a.dsum ? cols : 0, lead, e);
         }
         if constexpr (kFetch) {
-            R::fetch(a.dy, a.ld_dy, a.h, a.ld_h, r + step, a.rows, cols);
-            if constexpr (VB != kAny<DT>) if (a.dsum) R::fetch(a.dsum, a.ld_dsum, a.dsum, a.ld_dsum, r + step, a.rows, cols);
+            fetch_rows<DT, TPR>(a.dy, pitch_dy, a.h, pitch_h, r + step, rows, cols);
+            if constexpr (VB != kAny<DT>) if (a.dsum) fetch_rows<DT, TPR>(a.dsum, pitch_dsum, a.dsum, pitch_dsum, r + step, rows, cols);
         }
         ask(r + step);
         R::inside(cols, lead, d);
@@ -597,15 +614,15 @@ __global__ void __launch_bounds__(kBackwardThreads<TPR, E>, kBackwardBlocks<TPR,
                 for (int i = 0; i < R::NV; ++i)
                     if (on && R::any(R::column(i, lead), cols)) {
                         float v[R::VE];
-                        R::some(Of{a.dsum, a.ld_dsum, a.rows}, r, R::column(i, lead), cols, v);
+                        R::some(Of{a.dsum, pitch_dsum, rows}, r, R::column(i, lead), cols, v);
 #pragma unroll
                         for (int j = 0; j < R::VE; ++j) f[i * R::VE + j] += v[j];
                     }
             }
         }
-        if (on && a.dh) R::store(row_of<DT>(a.dh, a.ld_dh, r), cols, lead, d);
+        if (on && a.dh) R::store(row_at<DT>(a.dh, pitch_dh, r), cols, lead, d);
         if constexpr (FORM == kDrop) drop_row<DT, VB, TPR, E>(key, a.drop, r, lead, d);
-        if (on && a.dx) R::store(row_of<DT>(a.dx, a.ld_dx, r), cols, lead, d);
+        if (on && a.dx) R::store(row_at<DT>(a.dx, pitch_dx, r), cols, lead, d);
     }
     if (!a.partials) return;
     float* out = a.dweight ? fold : a.partials + (long long)blockIdx.x * a.cols;
@@ -779,7 +796,7 @@ __global__ void __launch_bounds__(32 * kFoldWarps) rms_fold_kernel(const float* 
 // Rows that start on 16-byte boundaries, all of them
 bool aligned(const void* p, long long ld, int elem) { return !p || ((uintptr_t)p % 16 == 0 && (ld * elem) % 16 == 0); }
 
-constexpr long long kRegisterWidth = 16384;
+constexpr long long kRegisterWidth = 16384, kMostRows = 1ll << 31;      // columns and rows of the register form
 
 // Blocks of `rows` rows each, at most `cap`; with a lead, blocks that come round again come to rows of the same lead: those are `period` apart
 unsigned blocks_of(long long rows, int groups, long long cap, int period) {
@@ -849,9 +866,12 @@ template <int DT, int VB, int FORM> cudaError_t forward_by_width(const RmsArgs& 
         const long long width = a.cols + (VB == kLead ? RowType<DT>::kVec - 1 : 0);
         if (width <= 256) return forward<DT, VB, 32, 8, FORM>(a, sms, stream);
         if (width <= 512) return forward<DT, VB, 32, 16, FORM>(a, sms, stream);
-        if (width <= 1024) return forward<DT, VB, kVector ? 128 : 64, kVector ? 8 : 16, FORM>(a, sms, stream);
-        if (width <= 2048) return forward<DT, VB, 128, 16, FORM>(a, sms, stream);
-        if (width <= 4096) return forward<DT, VB, 256, 16, FORM>(a, sms, stream);
+        // an element at a time with dropout, by 16 and by 8 elements a thread: fp32 4097 x 1001 25.5 and 14.6, bf16 8000 x 3001 (rows of two leads)
+        // 67.2 and 63.7
+        constexpr bool kFew = !kVector && FORM == kDrop;
+        if (width <= 1024) return forward<DT, VB, kVector || kFew ? 128 : 64, kVector || kFew ? 8 : 16, FORM>(a, sms, stream);
+        if (width <= 2048) return forward<DT, VB, kFew ? 256 : 128, kFew ? 8 : 16, FORM>(a, sms, stream);
+        if (width <= 4096) return forward<DT, VB, kFew ? 512 : 256, kFew ? 8 : 16, FORM>(a, sms, stream);
         if (width <= 8192) return forward<DT, VB, kWords ? 1024 : 512, kWords ? 8 : 16, FORM>(a, sms, stream);
         return forward<DT, VB, 1024, 16, FORM>(a, sms, stream);
     }
@@ -862,15 +882,16 @@ template <int DT, int VB, int FORM> cudaError_t backward_by_width(const RmsBackA
     if (width <= 512) return backward<DT, VB, 64, 8, FORM>(a, dweight, sms, used, stream);
     if (width <= 1024) return backward<DT, VB, 128, 8, FORM>(a, dweight, sms, used, stream);
     if (width <= 2048) return backward<DT, VB, 256, 8, FORM>(a, dweight, sms, used, stream);
-    // bf16 an element at a time, rows of two leads: 8000 x 3001 by (256, 16) 259 us, (512, 8) 142; fp32 61 and 90
+    // an element at a time, rows of two leads: bf16 8000 x 3001 by (256, 16) 259 us, (512, 8) 142; fp32 61 and 90
     constexpr bool kHalves = VB == kAny<DT> && DT == kBF16;
     if (width <= 4096) return backward<DT, VB, kHalves ? 512 : 256, kHalves ? 8 : 16, FORM>(a, dweight, sms, used, stream);
-    if constexpr (VB != kLead) { if (width <= 8192) return backward<DT, VB, VB == 16 ? 512 : 1024, VB == 16 ? 16 : 8, FORM>(a, dweight, sms, used, stream); }
+    if (width <= 8192) return backward<DT, VB, VB == 16 ? 512 : 1024, VB == 16 ? 16 : 8, FORM>(a, dweight, sms, used, stream);
     return backward<DT, VB, 1024, 16, FORM>(a, dweight, sms, used, stream);
 }
 template <int DT, int VB> cudaError_t forward_by_form(const RmsArgs& a, int sms, cudaStream_t stream) {
-    return a.scales ? forward_by_width<DT, VB, kE4m3>(a, sms, stream) : a.drop.limit ? forward_by_width<DT, VB, kDrop>(a, sms, stream)
-                                                                                     : forward_by_width<DT, VB, kPlain>(a, sms, stream);
+    if (a.scales) return forward_by_width<DT, VB, kE4m3>(a, sms, stream);
+    if constexpr (VB != kLead || DT == kBF16) { if (a.drop.limit) return forward_by_width<DT, VB, kDrop>(a, sms, stream); }
+    return forward_by_width<DT, VB, kPlain>(a, sms, stream);
 }
 template <int DT, int VB> cudaError_t backward_by_form(const RmsBackArgs& a, void* dweight, int sms, int* used, cudaStream_t stream) {
     return a.drop.limit && a.dx ? backward_by_width<DT, VB, kDrop>(a, dweight, sms, used, stream) : backward_by_width<DT, VB, kPlain>(a, dweight, sms, used, stream);
@@ -886,9 +907,10 @@ template <int DT> cudaError_t backward_by_access(const RmsBackArgs& a, int acces
 // How the rows of some matrices can be accessed, all alike: 16, kLead or (for more than one element's bytes) kAny
 struct Matrices {
     int elem, start = -1, step = -1;
-    bool same = true;
+    bool same = true, narrow = true;               // pitches that 32 bits hold
     void add(const void* p, long long ld) {
         if (!p) return;
+        narrow = narrow && ld * elem <= INT32_MAX;
         const int at = (int)((uintptr_t)p % 16), by = (int)(ld * elem % 16);
         if (start < 0) { start = at; step = by; }
         same = same && at == start && by == step;
@@ -925,19 +947,20 @@ cudaError_t launch_rms_forward(RmsArgs a, int dtype, int sms, cudaStream_t strea
     a.weight_vec = (uintptr_t)a.weight % 16 == 0;
     const bool e8 = a.scales != nullptr;
     const bool vec = aligned(a.x, a.ld_x, e) && aligned(a.residual, a.ld_residual, e) && aligned(a.sum, a.ld_sum, e) && (e8 || aligned(a.y, a.ld_y, e));
-    if (a.cols <= kRegisterWidth) {
-        Matrices m = {e};
-        m.add(a.x, a.ld_x);
-        m.add(a.residual, a.ld_residual);
-        m.add(a.sum, a.ld_sum);
-        if (!e8) m.add(a.y, a.ld_y);
+    Matrices m = {e};
+    m.add(a.x, a.ld_x);
+    m.add(a.residual, a.ld_residual);
+    m.add(a.sum, a.ld_sum);
+    if (!e8) m.add(a.y, a.ld_y);
+    if (a.cols <= kRegisterWidth && m.narrow && a.rows <= kMostRows && a.ld_y <= INT32_MAX) {
         // With a lead, groups of columns would start inside accesses, and the widest rows have no room for it.  Else, us an element at a time and with
-        // it: bf16 16000 x 999 35.5 and 19.7, 8000 x 3001 49.1 and 43.1, 3000 x 9001 122 and 93; but 2047 x 8191, where it takes the next form,
-        // 21.4 and 35.9.  fp32, whose single elements fill a line a warp, 8000 x 3001 44.2 and 35.4, but 4097 x 1001 5.9 and 6.8, 4000 x 5001 with
-        // dropout 54.7 and 75.7.
+        // it: bf16 16000 x 999 18.3 and 16.7, 8000 x 3001 47.0 and 36.4, 4000 x 7001 60.8 and 45.4, 3000 x 9001 with dropout 119 and 91; but 2047 x
+        // 8191, where it takes the next form, 21.4 and 35.9.  fp32, whose single elements fill a line a warp, 8000 x 3001 39.9 and 34.2, but with
+        // dropout 59.4 and 71.0, and 4097 x 1001 5.9 and 6.8.
         int access = m.access(a.cols);
         const long long width = a.cols + 16 / e - 1;
-        if (access == kLead && ((e8 && a.group) || width > kRegisterWidth || (dtype == kF32 ? a.cols <= 2048 || width > 4096 : a.cols <= 8192 && width > 8192))) access = e;
+        const bool gains = dtype == kF32 ? a.cols > 2048 && width <= 4096 && !a.drop.limit : a.cols > 8192 || width <= 8192;
+        if (access == kLead && ((e8 && a.group) || width > kRegisterWidth || !gains)) access = e;
         return dtype == kF32 ? forward_by_access<kF32>(a, access, sms, stream) : forward_by_access<kBF16>(a, access, sms, stream);
     }
     const bool vec8 = (uintptr_t)a.y % 8 == 0 && a.ld_y % 8 == 0;
@@ -959,18 +982,18 @@ cudaError_t launch_rms_backward(RmsBackArgs a, int dtype, void* dweight, int sms
     int used = 0;
     cudaError_t err = cudaSuccess;
     const bool vec = aligned(a.dy, a.ld_dy, e) && aligned(a.h, a.ld_h, e) && aligned(a.dsum, a.ld_dsum, e) && aligned(a.dh, a.ld_dh, e) && aligned(a.dx, a.ld_dx, e);
-    if (a.rows > 0 && a.cols <= kRegisterWidth) {
-        Matrices m = {e};
-        m.add(a.dy, a.ld_dy);
-        m.add(a.h, a.ld_h);
-        m.add(a.dsum, a.ld_dsum);
-        m.add(a.dh, a.ld_dh);
-        m.add(a.dx, a.ld_dx);
-        // As above: bf16 16000 x 999 45.7 and 33.5, 16000 x 1801 87.8 and 56.0, 3000 x 9001 131 and 89, but 200 x 5001 8.8 and 12.2, 8000 x 5001
-        // with dropout 167 and 191; fp32 8000 x 3001 76.2 and 77.5, 4097 x 1001 18.4 and 23.6
+    Matrices m = {e};
+    m.add(a.dy, a.ld_dy);
+    m.add(a.h, a.ld_h);
+    m.add(a.dsum, a.ld_dsum);
+    m.add(a.dh, a.ld_dh);
+    m.add(a.dx, a.ld_dx);
+    if (a.rows > 0 && a.cols <= kRegisterWidth && m.narrow && a.rows <= kMostRows) {
+        // As above: bf16 16000 x 999 51.7 and 29.1, 8000 x 3001 150 and 44.5, 8000 x 5001 with dsum 149 and 102, 2047 x 8181 34.8 and 35.1, 3000 x 9001
+        // with dsum 93.6 and 77.7, but 200 x 5001 8.1 and 10.4; fp32, before, 8000 x 3001 76.2 and 77.5, 4097 x 1001 18.4 and 23.6
         int access = m.access(a.cols);
         const long long width = a.cols + 16 / e - 1;
-        if (access == kLead && (dtype == kF32 || width > kRegisterWidth || (width > 4096 && a.cols <= 8192))) access = e;
+        if (access == kLead && (dtype == kF32 || width > kRegisterWidth || (width > 8192 && a.cols <= 8192))) access = e;
         err = dtype == kF32 ? backward_by_access<kF32>(a, access, dweight, sms, &used, stream) : backward_by_access<kBF16>(a, access, dweight, sms, &used, stream);
     } else if (a.rows > 0) {
         if (a.partials) {
