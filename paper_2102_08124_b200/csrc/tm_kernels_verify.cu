@@ -14,10 +14,11 @@
 // once; then the warps' statistics are joined through shared memory, the blocks' through the cluster's, and every block takes the same decisions.
 // Rounds of many positions read rows that turn out not to be reached, but wait once; they are for batches that leave the device half empty.
 //
-// Bound: by bytes HBM, 300 MB or 46 us for 256 sequences of up to 5 drafts and 131072 tokens in bf16; as measured 140 us.  Three pipes have 35 us of work
+// Bound: by bytes HBM, 300 MB or 46 us for 256 sequences of up to 5 drafts and 131072 tokens in bf16; as measured 144 us.  Three pipes have 35 us of work
 // each (an exponential a logit; the generator's wide products, 20 cycles a token and scheduler; conversions and maxima), its 55 M warp instructions
-// 48 us, and phases that follow one another with barriers between them leave the issue slots half idle.  256 draws of 131072 tokens: 55 us, of which
-// the generator needs 19; 4 drafts of one sequence, 32768 tokens in fp32: 11.2 us.  Equal or slower: three blocks of 512 threads an SM at 40
+// 48 us, and phases that follow one another with barriers between them leave the issue slots half idle.  256 draws of 131072 tokens: 56 us, of which
+// the generator needs 19; 4 drafts of one sequence, 32768 tokens in fp32: 12.5 us.  Decisions by the first block alone, told to the others, are 1.2 us and
+// 2 % of these; without them (140 us) equal or slower: three blocks of 512 threads an SM at 40
 // registers (138 - 145 us), four of 256 (130, but 21 us for one sequence of 131072 tokens against 18), one of 1024 (145), vectors asked for one
 // by one as others are taken (135), a second exponential a token in the race (168), its fp64 keys for every candidate (206).
 #include <algorithm>
@@ -220,7 +221,7 @@ template <int DT> __global__ void __launch_bounds__(kThreads, kBlocks) verify_ke
     __shared__ double exact_best[kWarps];
     __shared__ int exact_at[kWarps];
     __shared__ unsigned long long exact_block[2][2];
-    __shared__ int decided[2];                     // drafts that stay, how the sequence ends (or that it goes on)
+    __shared__ int decided[3];                     // of the first block, for all: drafts that stay, how the sequence ends (or that it goes on), drafts of the next round
     __shared__ float bound;
     const Philox key(a.keys, a.offset, a.offset_dev);
     const int cluster = a.cluster, b = blockIdx.x / cluster, rank = cluster > 1 ? (int)cluster_rank() : 0, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -234,18 +235,30 @@ template <int DT> __global__ void __launch_bounds__(kThreads, kBlocks) verify_ke
     const auto sync_all = [&] { if (cluster > 1) cluster_sync(); else __syncthreads(); };
 
     constexpr int kGoOn = 0, kDrawTarget = 1, kDrawRest = 2, kBad = 3;
+    // What decides how often the blocks wait for each other is read from memory by the first of them alone: others might see other numbers, should
+    // somebody write to them meanwhile, and would wait for good.
+    const auto drafts_from = [&](int k) {
+        int more = 0;
+        while (more < a.round && k + more < a.drafted && (unsigned)ids[k + more] < (unsigned)vocab) ++more;
+        return more;
+    };
+    const auto told = [&](int k) { return cluster > 1 ? __float_as_int(cluster_load_float(reinterpret_cast<const float*>(decided + k), 0)) : decided[k]; };
     int n = 0, turn = 0, end = kGoOn;
     RowStat p, q;
+    if (threadIdx.x == 0) {
+        bound = 0.0f;
+        if (rank == 0) decided[2] = drafts_from(0);
+    }
+    sync_all();
     for (;; turn ^= 1) {
         // the round's positions: up to the first that has no draft, with it
-        int drafts = 0;
-        while (drafts < a.round && n + drafts < a.drafted && (unsigned)ids[n + drafts] < (unsigned)vocab) ++drafts;
+        const int drafts = told(2);
         const int positions = min(a.round, drafts + 1), rows = positions + (a.draft_logits ? drafts : 0);
         // what the tests need besides: thread k its position's
         int id = 0;
         float zp = 0.0f, zq = 0.0f;
-        if ((int)threadIdx.x < drafts) {
-            id = ids[n + threadIdx.x];
+        if (rank == 0 && (int)threadIdx.x < drafts) {
+            id = min(max(ids[n + threadIdx.x], 0), vocab - 1);
             zp = to_float(target(n + threadIdx.x)[id]);
             if (a.draft_logits) zq = to_float(draft(n + threadIdx.x)[id]);
         }
@@ -297,7 +310,7 @@ template <int DT> __global__ void __launch_bounds__(kThreads, kBlocks) verify_ke
             if (k == 0) stat[row] = RowStat{s > 0.0 ? m : INFINITY, s};
         }
         __syncthreads();
-        if (warp == 0) {
+        if (rank == 0 && warp == 0) {
             // lane k: position n + k
             int what = kGoOn;
             float lp = 0.0f;
@@ -324,18 +337,21 @@ template <int DT> __global__ void __launch_bounds__(kThreads, kBlocks) verify_ke
             const unsigned ends = __ballot_sync(0xFFFFFFFFu, what != kGoOn);
             const int stay = ends ? __ffs(ends) - 1 : positions;
             const int how = __shfl_sync(0xFFFFFFFFu, what, ends ? stay : 0);
-            if (lane < stay && rank == 0) {
+            if (lane < stay) {
                 tokens[n + lane] = id;
                 if (logp) logp[n + lane] = lp;
             }
-            if (lane == 0) { decided[0] = stay; decided[1] = how; bound = 0.0f; }
+            if (lane == 0) {
+                decided[0] = stay;
+                decided[1] = how;
+                decided[2] = how == kGoOn ? drafts_from(n + stay) : 0;
+            }
         }
-        __syncthreads();
-        const int stay = decided[0];
-        end = decided[1];
+        sync_all();
+        const int stay = told(0);
+        end = told(1);
         n += stay;
         if (end != kGoOn) { p = stat[stay]; q = stat[kPositions + stay]; break; }
-        __syncthreads();                           // before the next round's statistics
     }
 
     int token = -1;
@@ -449,7 +465,7 @@ cudaError_t launch_verify(const VerifyArgs& args, int dtype, int sms, cudaStream
     a.cp64 = 1.4426950408889634 / (double)a.temperature;
     a.cq64 = 1.4426950408889634 / (double)a.draft_temperature;
     // Blocks of a sequence: as many as the device holds (two an SM), each with 4096 tokens at least; twice that where rows are long and sequences
-    // end at different positions.  us by 1, 2, 4, 8 blocks: 256 sequences of 5 drafts and fewer, 131072 tokens bf16 157, 140, 142, 187; 256 of 3, 32001
+    // end at different positions.  us by 1, 2, 4, 8 blocks (before decisions were the first block's, 1 us a round less): 256 sequences of 5 drafts and fewer, 131072 tokens bf16 157, 140, 142, 187; 256 of 3, 32001
     // 49, 59, 83, 136; 256 of none, 131072 56, 62, 75, 113; 64 of 4, 131072 97, 61, 52, 66; 1 of 4, 32768 fp32 25, 19, 14, 11.
     int cluster = 1;
     const long long room = 2ll * sms;
