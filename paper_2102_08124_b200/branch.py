@@ -64,7 +64,11 @@ def _make():
                 dy = torch.zeros_like(h)
             dh, dx, dw = bb.tm_rms_norm_backward(_rows(dy), h, rstd, weight, dsum=None if dsum is None else _rows(dsum), p=p, seed=seed, offset=offset,
                                                  offset_dev=offset_dev, want_dh=need[1], want_weight=need[2])
-            return (dx.view(ctx.shape) if need[0] else None, dh.view(ctx.shape) if need[1] else None, dw) + (None,) * 5
+            # with p = 0 both are one tensor, and stay one: autograd copies a tensor that it gets twice, but not two views of it
+            one = dh is dx
+            dx = dx.view(ctx.shape)
+            dh = dx if one else dh.view(ctx.shape) if need[1] else None
+            return (dx if need[0] else None, dh if need[1] else None, dw) + (None,) * 5
 
     return Dropout, Norm
 
