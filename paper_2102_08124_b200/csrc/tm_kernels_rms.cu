@@ -112,6 +112,9 @@ struct Divide {
     __device__ __forceinline__ uint32_t operator()(uint32_t x) const { return (uint32_t)(((unsigned long long)x * m) >> (31 + shift)); }
 };
 
+// What is added where there is no residual: -0, which leaves a zero its sign
+template <int DT> constexpr uint32_t kNothing = DT == kF32 ? 0x80000000u : 0x80008000u;
+
 // A thread a block of eight columns (16 bytes of bf16; twice that of fp32, the last half perhaps past the row), kEach of them at a time
 constexpr int kDropThreads = 256, kDropBlocks = 5;
 template <int DT, bool DROP> __global__ void __launch_bounds__(kDropThreads, kDropBlocks) dropout_kernel(const DropoutArgs a, const Divide by, uint32_t all) {
@@ -129,7 +132,8 @@ template <int DT, bool DROP> __global__ void __launch_bounds__(kDropThreads, kDr
             c[k] = (i - r[k] * by.d) * 8;
 #pragma unroll
             for (int q = 0; q < N; ++q) {
-                x[k][q] = s[k][q] = make_uint4(0, 0, 0, 0);
+                x[k][q] = make_uint4(0, 0, 0, 0);
+                s[k][q] = make_uint4(kNothing<DT>, kNothing<DT>, kNothing<DT>, kNothing<DT>);
                 if (i < all && (int)c[k] + q * V < cols) {
                     x[k][q] = *reinterpret_cast<const uint4*>(row_of<DT>(a.x, a.ld_x, r[k]) + c[k] + q * V);
                     if (a.residual) s[k][q] = *reinterpret_cast<const uint4*>(row_of<DT>(a.residual, a.ld_residual, r[k]) + c[k] + q * V);
@@ -175,7 +179,7 @@ template <int DT> __global__ void __launch_bounds__(kDropThreads) dropout_any_ke
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             v[j] = 32 * j < left ? to_float(x[32 * j]) : 0.0f;
-            w[j] = s && 32 * j < left ? to_float(s[32 * j]) : 0.0f;
+            w[j] = s && 32 * j < left ? to_float(s[32 * j]) : -0.0f;
         }
         const uint32_t kept = a.drop.limit ? kept_bits(key((uint32_t)(c0 / 8) + lane, (uint32_t)r), a.drop.limit) : 0xFFu;
 #pragma unroll
