@@ -11,39 +11,46 @@ from . import binding_branch as bb
 from .distill import train
 
 
-def draw(logits, seed: int, offset: int = 0, temperature: float = 1.0):
-    """One token from softmax(logits / temperature) of every row (int32 [rows])."""
+def draw(logits, seed: int, offset: int = 0, temperature: float = 1.0, status=None):
+    """One token from softmax(logits / temperature) of every row (int32 [rows]); -1 where a row holds NaN, +Inf or nothing but -Inf, which `status`
+    (int32[1] or None) shows too."""
     import torch
     none = torch.empty((logits.shape[0], 0), dtype=torch.int32, device=logits.device)
-    return bb.tm_verify_draft(logits, None, none, seed, offset, temperature=temperature, want_logp=False)[0][:, 0]
+    return bb.tm_verify_draft(logits, None, none, seed, offset, temperature=temperature, want_logp=False, status=status)[0][:, 0]
 
 
 def speculate(target, drafter, last, drafts: int, seed: int, offset: int = 0, temperature: float = 1.0, status=None):
     """One round for sequences whose last tokens are `last` [batch]: `drafts` tokens from the drafter, one after the other, then the target's
     check of all of them.  target and drafter map tokens [n] to the next token's logits [n, vocab].  Takes drafts + 1 offsets.
-    Returns (tokens [batch, drafts + 1], accepted [batch]): the drafts that stayed, one more token, and -1 behind it."""
+    Returns (tokens [batch, drafts + 1], accepted [batch]): the drafts that stayed, one more token, and -1 behind it.
+    A sequence has ended where its last token is negative, as it is behind a row of the target's that nothing can be drawn from: it stays
+    at -1.  A row of the drafter's of that kind ends the sequence's drafts of the round.  Negative tokens reach neither network (token 0 does, and
+    its logits are not used).  status: shows such rows, the drafter's too."""
     import torch
     tokens, rows = [last], []
     for i in range(drafts):
-        rows.append(drafter(tokens[-1]))
-        tokens.append(draw(rows[-1], seed, offset + i, temperature))
+        rows.append(drafter(tokens[-1].clamp_min(0)))
+        tokens.append(torch.where(tokens[-1] < 0, -1, draw(rows[-1], seed, offset + i, temperature, status)))
     given = torch.stack(tokens, 1)                                       # [batch, drafts + 1]
-    logits = target(given.reshape(-1))
+    logits = target(given.clamp_min(0).reshape(-1))
     draft_logits = torch.stack(rows, 1).reshape(-1, logits.shape[1]) if drafts else None
     out, accepted, _ = bb.tm_verify_draft(logits, draft_logits, given[:, 1:].contiguous().int(), seed, offset + drafts, temperature=temperature,
                                           want_logp=False, status=status)
-    return out, accepted
+    return torch.where(last[:, None] < 0, -1, out), accepted
 
 
 def share_that_stays(target, drafter, last, drafts: int, rounds: int, seed: int, temperature: float = 1.0) -> float:
     """Share of the tested drafts that stayed, over `rounds` rounds."""
     import torch
     kept = tested = 0
+    status = torch.zeros(1, dtype=torch.int32, device=last.device)
     for i in range(rounds):
-        out, accepted = speculate(target, drafter, last, drafts, seed, i * (drafts + 1), temperature)
+        out, accepted = speculate(target, drafter, last, drafts, seed, i * (drafts + 1), temperature, status)
         last = out.gather(1, accepted.long()[:, None])[:, 0]
         kept += int(accepted.sum())
         tested += int((accepted + (accepted < drafts)).sum())
+    if int(status):
+        raise FloatingPointError("a row of logits holds NaN, +Inf or nothing but -Inf")
     return kept / max(tested, 1)
 
 
