@@ -148,28 +148,29 @@ class Blocks:
             setattr(other, name, [p.detach().clone().requires_grad_() for p in getattr(self, name)])
         return other
 
-    def _norm(self, i, update, h, p, seed, offset):
+    def _norm(self, i, update, h, p, seed, offset, offset_dev):
         """Norm i of h + dropout(update): (y, the sum)."""
         if self.norm == "rms":
             return rms_norm(h if update is None else update, self.norm_weight[i], residual=None if update is None else h, p=0.0 if update is None else p,
-                            seed=seed, offset=offset + i)
+                            seed=seed, offset=offset + i, offset_dev=offset_dev)
         if update is not None and p > 0:
-            h, update = dropout(update, p, seed, offset + i, residual=h), None
+            h, update = dropout(update, p, seed, offset + i, residual=h, offset_dev=offset_dev), None
         return layer_norm(h if update is None else update, self.norm_weight[i], self.norm_bias[i], residual=None if update is None else h)
 
-    def logits(self, tokens, masked: Optional[list] = None, p: float = 0.0, seed: int = 0, offset: int = 0):
+    def logits(self, tokens, masked: Optional[list] = None, p: float = 0.0, seed: int = 0, offset: int = 0, offset_dev=None):
         """masked: the linear layers' masked weights; None runs the dense ones.  p: dropout of the blocks' outputs, from seed and as many offsets as
-        there are norms."""
+        there are norms.  offset_dev (int64[1] on the device, or None) is added to them when the kernels run: for a captured step, which raises it by
+        that many behind its backward pass."""
         import torch
         h, update = self.embedding[tokens], None
         for i in range(len(self.linear) // 2):
-            y, h = self._norm(i, update, h, p, seed, offset)
+            y, h = self._norm(i, update, h, p, seed, offset, offset_dev)
             a, b = self.linear[2 * i], self.linear[2 * i + 1]
             if masked is None:
                 update = torch.nn.functional.gelu(y @ a.t()) @ b.t()
             else:
                 update = masked_linear(torch.nn.functional.gelu(masked_linear(y, a, masked[2 * i])), b, masked[2 * i + 1])
-        y, _ = self._norm(len(self.linear) // 2, update, h, p, seed, offset)
+        y, _ = self._norm(len(self.linear) // 2, update, h, p, seed, offset, offset_dev)
         return y @ self.head.t()
 
 
