@@ -12,7 +12,7 @@ _functions = None
 
 def _rows(t):
     """As a matrix whose rows lie apart from each other, copied if need be (the gradient of a sum is an expanded scalar or row)."""
-    t = t.reshape(-1, t.shape[-1])
+    t = t.reshape(t.shape[:-1].numel(), t.shape[-1])                     # not -1, which tensors without columns do not tell
     apart = (t.shape[1] <= 1 or t.stride(1) == 1) and (t.shape[0] <= 1 or t.stride(0) >= t.shape[1])
     return t if apart else t.contiguous()
 
@@ -59,7 +59,7 @@ def _make():
             need = ctx.needs_input_grad
             if dy is None and dsum is None:
                 return (None,) * 8
-            h = h.view(-1, h.shape[-1])
+            h = _rows(h)
             if dy is None:                                  # only the sum was used
                 dy = torch.zeros_like(h)
             dh, dx, dw = bb.tm_rms_norm_backward(_rows(dy), h, rstd, weight, dsum=None if dsum is None else _rows(dsum), p=p, seed=seed, offset=offset,

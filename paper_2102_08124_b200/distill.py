@@ -56,7 +56,7 @@ def _make():
         @once_differentiable
         def backward(ctx, dy, dsum):
             h, mean, rstd, weight = ctx.saved_tensors
-            h = h.view(-1, h.shape[-1])
+            h = _rows(h)
             want = ctx.params[0] and any(ctx.needs_input_grad[2:4])
             dsum = None if dsum is None else _rows(dsum)
             if dy is None:                                  # only the sum was used
