@@ -337,12 +337,14 @@ int tm_distill_loss_grad(const void* logits, int dtype, int64_t rows, int64_t vo
  * tm_rms_norm -- h = d(x) + residual (p = 0: d(x) = x; residual NULL: none); over the columns of every row
  * rstd = 1 / sqrt(mean(h^2) + eps), y = h * rstd * weight (cols entries of weight_dtype, NULL for ones).  sum_out (may be NULL) receives h
  * rounded to dtype, rstd_out (rows floats, may be NULL) rstd; y comes from h before rounding.  y or sum_out may lie on x or residual.
- * The squares are summed in fp32 (magnitudes up to 2^63 / sqrt(cols)).  With cols 0 nothing is written.
+ * The squares are summed in fp32 (magnitudes up to 2^63 / sqrt(cols)), and h * weight is formed before rstd is (it has to lie in fp32's range too).
+ * With cols 0 nothing is written.
  *
  * tm_rms_norm_e4m3 -- the same without dropout, y in 8 bits (e4m3: four bits of exponent, three of mantissa, largest value 448) with a scale for
  * every `group` columns of a row (32, 64 or 128; the last may have fewer; 0: one for the row): scale = max(max |y| / 448, 2^-126),
- * y8 = y / scale rounded to nearest even; y is scale * y8.  scales_out[rows][ceil(cols / group)] (group 0: [rows]).  NaN stays NaN in y8 and has no
- * part in the scale.  sum_out may lie on x or residual, y8 on neither.
+ * y8 = y / scale rounded to nearest even, quotients being products with inverses in fp32: y / scale is off by a few units (2^-24) before it is rounded, so
+ * a value that near the middle between two numbers of 8 bits may go to either; y is scale * y8.  scales_out[rows][ceil(cols / group)] (group 0:
+ * [rows]).  NaN stays NaN in y8 and has no part in the scale.  sum_out may lie on x or residual, y8 on neither.
  *
  * tm_rms_norm_backward -- with g = dy * weight and xh = h * rstd:
  *   dh = rstd * (g - xh * mean_c(g * xh)) + dsum,   dx = d(dh) (the forward pass's p, seed and offsets),   dweight = sum_r(dy * xh).
@@ -381,8 +383,9 @@ int tm_rms_norm_backward(const void* dy, int64_t ld_dy, const void* h, int64_t l
  * -Inf (a masked logit) has probability 0.  A row that is reached and holds NaN, +Inf or nothing but -Inf ends its sequence with
  * token -1 and logp NaN and raises TM_DEV_NONFINITE in *status_dev (may be NULL); an id that is not below vocab ends the drafts like a negative
  * one and raises TM_DEV_BADID.  Rows behind the first refused draft have no part in the answer (they may be read).  The sums of a row are fp32 sums
- * joined in fp64: p and q hold them to some 2^-23, so p - q counts as 0 where log2 p - log2 q is 2^-20 or less; comparisons that fp32 cannot tell
- * are made in fp64.  Tokens below 2^-126 of the row's largest p are not drawn.  1 <= vocab <= TM_VOCAB_MAX, 0 <= drafted <= TM_DRAFT_MAX.
+ * joined in fp64, some 2^-21 off (2^-16 at 131072 tokens, should all roundings go the same way), and p and q with them; p - q counts as 0 where log2 p -
+ * log2 q is 2^-20 or less; comparisons that fp32 cannot tell are made in fp64.  Tokens below 2^-126 of the row's largest p are not drawn.
+ * 1 <= vocab <= TM_VOCAB_MAX, 0 <= drafted <= TM_DRAFT_MAX.
  */
 #define TM_DRAFT_MAX 1024
 int tm_verify_draft(const void* logits, int dtype, int64_t batch, int64_t drafted, int64_t vocab, int64_t ld, const void* draft_logits,

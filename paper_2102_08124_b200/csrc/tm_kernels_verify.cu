@@ -17,7 +17,9 @@
 // Bound: by bytes HBM, 300 MB or 46 us for 256 sequences of up to 5 drafts and 131072 tokens in bf16; as measured 144 us.  Three pipes have 35 us of work
 // each (an exponential a logit; the generator's wide products, 20 cycles a token and scheduler; conversions and maxima), its 55 M warp instructions
 // 48 us, and phases that follow one another with barriers between them leave the issue slots half idle.  256 draws of 131072 tokens: 56 us, of which
-// the generator needs 19; 4 drafts of one sequence, 32768 tokens in fp32: 12.5 us.  Decisions by the first block alone, told to the others, are 1.2 us and
+// the generator needs 19; 4 drafts of one sequence, 32768 tokens in fp32: 12.5 us, by the eight blocks that a cluster has at most.  Without the
+// drafter's logits: 256 sequences of 5 drafts 127 us of 39, 64 of 4 39 of 9.  Two blocks of 512 leave a thread 64 registers, and what the statistics and
+// the race keep side by side spills 204 bytes (bf16) and 244 (fp32).  Decisions by the first block alone, told to the others, are 1.2 us and
 // 2 % of these; without them (140 us) equal or slower: three blocks of 512 threads an SM at 40
 // registers (138 - 145 us), four of 256 (130, but 21 us for one sequence of 131072 tokens against 18), one of 1024 (145), vectors asked for one
 // by one as others are taken (135), a second exponential a token in the race (168), its fp64 keys for every candidate (206).
@@ -34,10 +36,14 @@ constexpr uint32_t kTestBlocks = 0x80000000u;      // the generator's blocks of 
 constexpr int kThreads = 512, kBlocks = 2, kWarps = kThreads / 32, kMaxCluster = 8;
 constexpr int kPositions = 8, kRows = 2 * kPositions;      // of a round: the target's rows, then the drafter's
 constexpr int kLoads = 4;                          // 16-byte vectors that a lane asks for at once: a segment of a row is 32 kLoads of them
-// What fp32 may be off by, relative: probabilities by kOff (an exponential has 2^-22, its exponent's roundings 126 * 2^-23 each), keys of the race by
-// less than half of kNear.  What is closer than kNear is told apart in fp64.
+// What fp32 may be off by, relative.  A probability: 2^-22 of the exponential, and three roundings of an exponent of 126 at most (difference, c, product), 3 *
+// 126 * 2^-24 ln 2 = 1.6e-5; kOff is above it.  1 / E: 2^-15 (race_gain).  A key has both, 5e-5, which is below half of kNear: keys further apart than kNear
+// are in the right order, and nearer ones are told apart in fp64.
 constexpr float kOff = 6e-5f, kNear = 4e-4f;
-// log2 p - log2 q up to which p - q counts as nothing: the rows' sums are fp32 sums, so p and q of equal rows may differ by some 2^-23
+// log2 p - log2 q up to which p - q counts as nothing.  The rows' sums are fp32 sums: a thread adds up to vocab / 512 numbers (where one block
+// has the sequence; an eighth of that where eight have; 128 where all positions are one round) one after the other, each addition off by 2^-24 at
+// most, so 131072 tokens have 2^-16 if all were off the same way, and some 2^-21 as they fall.  Rows that are equal but for that then differ by one
+// factor in all tokens: p - q is nothing, or p times a constant, and both mean a draw from p.
 constexpr double kEqual = 0x1p-20;
 constexpr float kSlack = 1e-3f;                    // of a logarithm in the race's screening, eight of its units
 
@@ -108,7 +114,8 @@ __device__ __noinline__ double race_key(double x, double y, uint32_t word) {
     const double r = x - y > kEqual ? exp2(x) - exp2(y) : 0.0;
     return r > 0.0 ? r / -log1p(-((double)word + 0.5) * 0x1p-32) : 0.0;
 }
-// 1 / E in fp32, good to 2^-20: u = (word + 1/2) / 2^32 near 0 by E's series, else by the logarithm of 1 - u
+// 1 / E in fp32, u = (word + 1/2) / 2^32.  Near 0 by E's series (its next term is 2^-26 of it).  Else by the logarithm of 1 - u, which __log2f has to 2^-22
+// and 1 - u itself to 2^-24, absolute: at u = 1/64, where E is least, 2^-16.5 and 2^-18 of E.  So 2^-15 with the product and the quotient, and better from there on.
 __device__ __forceinline__ float race_gain(uint32_t word) {
     const float u = fmaf((float)word, 0x1p-32f, 0x1p-33f);
     const float e = u < 0.015625f ? u * fmaf(u, fmaf(u, fmaf(u, 0.25f, 0.33333333f), 0.5f), 1.0f) : -0.69314718f * __log2f(fmaf((float)~word, 0x1p-32f, 0x1p-33f));
@@ -464,8 +471,8 @@ cudaError_t launch_verify(const VerifyArgs& args, int dtype, int sms, cudaStream
     static_cast<VerifyArgs&>(a) = args;
     a.cp64 = 1.4426950408889634 / (double)a.temperature;
     a.cq64 = 1.4426950408889634 / (double)a.draft_temperature;
-    // Blocks of a sequence: as many as the device holds (two an SM), each with 4096 tokens at least; twice that where rows are long and sequences
-    // end at different positions.  us by 1, 2, 4, 8 blocks (before decisions were the first block's, 1 us a round less): 256 sequences of 5 drafts and fewer, 131072 tokens bf16 157, 140, 142, 187; 256 of 3, 32001
+    // Blocks of a sequence: as many as the device holds (two an SM), up to a portable cluster's eight, each with more than 2048 tokens; twice that where rows
+    // are long and sequences end at different positions.  us by 1, 2, 4, 8 blocks (before decisions were the first block's, 1 us a round less): 256 sequences of 5 drafts and fewer, 131072 tokens bf16 157, 140, 142, 187; 256 of 3, 32001
     // 49, 59, 83, 136; 256 of none, 131072 56, 62, 75, 113; 64 of 4, 131072 97, 61, 52, 66; 1 of 4, 32768 fp32 25, 19, 14, 11.
     int cluster = 1;
     const long long room = 2ll * sms;
